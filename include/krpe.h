@@ -312,6 +312,99 @@ krpe_status_t krpe_attention_bwd(const void* q, const void* k, const void* v, in
 krpe_status_t krpe_attention_fwd_stats(const void* ws, size_t ws_bytes, int B, int H, int n, int d, int m,
                                        unsigned* fixed_rows, void* stream);
 
+/*
+ * Attention with a bias that decays: b_t = rate t for t <= 0 and -inf after,
+ * one rate per head.  Eq. (10) then has a state of constant size,
+ *
+ *   [num_i | den_i] = A_i phi(q_i),  z_i = num_i / den_i,
+ *   A_i = e^{-rate} A_{i-1} + [v_i; 1] phi(k_i)^T     (A: [d + 1, M], its last row
+ *                                                      the denominators')
+ *
+ * so a prompt costs O(n), a token O(1).  The entry points below share:
+ * - rate : [H] fp32, >= 0 (inf: a position sees itself alone; below zero the past
+ *   grows, within fp32's range).
+ * - features: PRF of Eq. (5) or KRPE_FEAT_ELU (m == d, W not read), with KRPE_NPRF or
+ *   not; M = m.  No trigonometric features: their denominators can vanish, and
+ *   nothing here certifies a row (KRPE_ERR_UNSUPPORTED).
+ * - z and the gradients have the type of q, k, v.  Sums are fp32; operands of the matrix
+ *   products are three bf16 terms, an fp32 value whole, where the result is fp32 (the states
+ *   always), and one or two where it is rounded to bf16.
+ * - a pool of states: fp32 [nslots][H][d + 1][M].  slots (device, [B] int32, or NULL: sequence
+ *   b has slot b, nslots >= B) names each sequence's; -1: none, zeros before the call and not
+ *   kept after it.  A slot outside [-1, nslots), or one that two sequences of a call name, is
+ *   refused on the device: these sequences' z is NaN and the pool stays as it was.
+ * - features have to stay within fp32's range, as krpe_feature_map's.  A q, k or v element that
+ *   is not finite makes what sees it not finite, and nothing else (gradients: its whole sequence
+ *   and head).
+ * - rate and integer arrays need 4-byte alignment, all others 16 bytes.
+ * - 1 <= d <= 128, 1 <= m <= 1024; B H n < 2^31, no other limit of n.
+ */
+
+/*
+ * KRPE_STATE_FRESH (krpe_decay_fwd): sequences start from zeros; their slots are written only.
+ */
+#define KRPE_STATE_FRESH 64u
+
+/*
+ * Prompts: z [B, H, n, d] of q, k, v [B, H, n, d], in chunks of 128 positions.
+ * lens  : [B] int32 (device) or NULL: sequence b has min(max(lens[b], 0), n) positions; z
+ *         rows behind them stay as they were, q, k, v rows behind them weigh nothing.
+ * state : pool read before (not with KRPE_STATE_FRESH) and left as the states behind the
+ *         sequences, or NULL (zeros before, not kept; slots must be NULL and nslots 0).
+ * n == 0 is valid (it clears the slots with KRPE_STATE_FRESH).
+ */
+size_t krpe_decay_fwd_workspace(int B, int H, int n, int d, int m, unsigned flags);
+krpe_status_t krpe_decay_fwd(const void* q, const void* k, const void* v, int qkv_dtype, const float* rate,
+                             const float* W, void* z, float* state, const int* slots, int nslots, const int* lens,
+                             int B, int H, int n, int d, int m, unsigned flags, void* ws, size_t ws_bytes,
+                             void* stream);
+
+/*
+ * Backward pass of krpe_decay_fwd from zero states, W and rate fixed: dq, dk, dv [B, H, n, d] of
+ * L = sum(dz * z), all in qkv_dtype.  Rows behind lens stay as they were.  The forward pass is
+ * recomputed inside.
+ */
+size_t krpe_decay_bwd_workspace(int B, int H, int n, int d, int m, unsigned flags);
+krpe_status_t krpe_decay_bwd(const void* q, const void* k, const void* v, int qkv_dtype, const float* rate,
+                             const float* W, const void* dz, void* dq, void* dk, void* dv, const int* lens, int B,
+                             int H, int n, int d, int m, unsigned flags, void* ws, size_t ws_bytes, void* stream);
+
+/*
+ * One token of every sequence: the states take k, v [B, H, d] in, z [B, H, d] is q's row of Eq. (10).
+ */
+krpe_status_t krpe_decay_step(const void* q, const void* k, const void* v, int qkv_dtype, const float* rate,
+                              const float* W, void* z, float* state, const int* slots, int nslots, int B, int H,
+                              int d, int m, unsigned flags, void* stream);
+
+/*
+ * Trees of T <= 64 drafted tokens behind every sequence: node t of q, k, v [B, H, T, d] sees the
+ * state, its ancestors and itself; its distances are those along its path.
+ * parent : [B, T] int32 (device), parent[b][t] < t, -1 for a child of the sequence's last token.
+ *          A node with any other parent is none: its row of z is zero, and so are those below it.
+ * The states are read only: krpe_decay_commit takes the accepted nodes in.
+ */
+#define KRPE_TREE_MAX 64
+krpe_status_t krpe_decay_tree(const void* q, const void* k, const void* v, int qkv_dtype, const int* parent,
+                              const float* rate, const float* W, void* z, const float* state, const int* slots,
+                              int nslots, int B, int H, int T, int d, int m, unsigned flags, void* stream);
+
+/*
+ * Takes tokens path[b][0], path[b][1], .. of k, v [B, H, T, d] into the states, in that order, up
+ * to the first entry outside [0, T) or P entries.  path: [B, P] int32 (device).
+ */
+krpe_status_t krpe_decay_commit(const void* k, const void* v, int qkv_dtype, const int* path, const float* rate,
+                                const float* W, float* state, const int* slots, int nslots, int B, int H, int T,
+                                int P, int d, int m, unsigned flags, void* stream);
+
+/*
+ * state[dst[i]] = state[src[i]] for i < count <= KRPE_COPY_MAX, all at once: sources are as they
+ * were before the call, also where moves overlap; src -1 clears; of moves to one slot the last
+ * holds.  Moves with a slot outside the pool are left out.  src, dst: [count] int32 (device).
+ */
+#define KRPE_COPY_MAX 256
+krpe_status_t krpe_decay_state_copy(float* state, const int* src, const int* dst, int count, int nslots, int H, int d,
+                                    int m, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

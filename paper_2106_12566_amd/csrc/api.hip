@@ -7,19 +7,23 @@
 #include <mutex>
 #include <string>
 
+#include "api_util.hpp"
 #include "common.hpp"
 #include "krpe.h"
 #include "launch.hpp"
 
 namespace krpe {
 namespace {
-
 thread_local std::string g_last_error;
+}  // namespace
 
 krpe_status_t fail(krpe_status_t s, const std::string& msg) {
   g_last_error = msg;
   return s;
 }
+void clear_error() { g_last_error.clear(); }
+
+namespace {
 
 int log2_ceil(int n) {
   int l = 0;
@@ -27,31 +31,10 @@ int log2_ceil(int n) {
   return l;
 }
 
-size_t align_up(size_t v) { return (v + 255) & ~static_cast<size_t>(255); }
-
 // Bytes of an array of `rows` rows of N floats that the convolution reads as
 // phi rows, plus one row of slack: with buffer reads its loop loads one row
 // past a unit's last row (never used), which for the last unit lands here.
 size_t phi_bytes(size_t rows, size_t N) { return (rows + 1) * N * sizeof(float); }
-
-bool misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }
-
-struct Range {
-  const void* p;
-  size_t bytes;
-};
-bool overlaps(Range a, Range b) {
-  if (a.bytes == 0 || b.bytes == 0) return false;
-  const uintptr_t a0 = reinterpret_cast<uintptr_t>(a.p), b0 = reinterpret_cast<uintptr_t>(b.p);
-  return a0 < b0 + b.bytes && b0 < a0 + a.bytes;
-}
-
-size_t dtype_size(int dt) { return dt == KRPE_BF16 ? 2 : 4; }
-
-krpe_status_t hip_check(hipError_t e, const char* what) {
-  if (e == hipSuccess) return KRPE_OK;
-  return fail(KRPE_ERR_HIP, std::string(what) + ": " + hipGetErrorString(e));
-}
 
 krpe_status_t check_dims(int B, int H, int n, int d, int m, bool need_dm, int max_log2n = kMaxLog2N) {
   if (B < 0 || H < 0 || n < 0 || (need_dm && (d < 0 || m < 0))) return fail(KRPE_ERR_SHAPE, "negative size");
@@ -741,7 +724,7 @@ const char* krpe_last_error(void) { return g_last_error.c_str(); }
 
 krpe_status_t krpe_feature_map_ex(const void* x, int x_dtype, const float* W, float* phi, int B, int H, int n,
                                   int d, int m, unsigned flags, void* stream) {
-  g_last_error.clear();
+  clear_error();
   if (krpe_status_t s = check_dims(B, H, n, d, m, true, kMaxLongLog2N)) return s;
   int kind = kFeatPrf, M = m;
   if (krpe_status_t s = feature_kind(flags, d, m, &kind, &M)) return s;
@@ -778,13 +761,13 @@ size_t krpe_toeplitz_conv_workspace(int B, int H, int C, int n) {
 
 krpe_status_t krpe_toeplitz_conv(const float* b, const float* a, float* y, int B, int H, int C, int n, void* ws,
                                  size_t ws_bytes, void* stream) {
-  g_last_error.clear();
+  clear_error();
   return toeplitz_conv(b, a, y, B, H, C, n, ws, ws_bytes, stream);
 }
 
 krpe_status_t krpe_toeplitz_conv_noalloc(const float* b, const float* a, float* y, int B, int H, int C, int n,
                                          void* stream) {
-  g_last_error.clear();
+  clear_error();
   // sizes first (no HIP call for a rejected request), then the workspace
   if (C < 0) return fail(KRPE_ERR_SHAPE, "negative size");
   if (krpe_status_t s = check_dims(B, H, n, 0, 0, false, kMaxLongLog2N)) return s;
@@ -821,7 +804,7 @@ size_t krpe_attention_fwd_workspace(int B, int H, int n, int d, int m) {
 krpe_status_t krpe_attention_fwd_profiled(const void* q, const void* k, const void* v, int qkv_dtype, const float* b,
                                           const float* W, float* z, int B, int H, int n, int d, int m, unsigned flags,
                                           void* ws, size_t ws_bytes, void* stream, void* const* events) {
-  g_last_error.clear();
+  clear_error();
   if (krpe_status_t s = check_dims(B, H, n, d, m, true, kMaxLongLog2N)) return s;
   int kind = kFeatPrf, M = m;
   if (krpe_status_t s = feature_kind(flags, d, m, &kind, &M)) return s;
@@ -898,7 +881,7 @@ krpe_status_t krpe_attention_bwd(const void* q, const void* k, const void* v, in
                                  const float* W, const float* dz, float* dq, float* dk, float* dv, float* db, int B,
                                  int H, int n, int d, int m, unsigned flags, void* ws, size_t ws_bytes,
                                  void* stream) {
-  g_last_error.clear();
+  clear_error();
   if (krpe_status_t s = check_dims(B, H, n, d, m, true)) return s;
   if (flags & ~kBwdFlags)
     return fail(KRPE_ERR_UNSUPPORTED, "the backward pass takes KRPE_NPRF, the route bits and KRPE_HINT_CAUSAL (PRF features)");
@@ -1029,7 +1012,7 @@ krpe_status_t krpe_attention_bwd(const void* q, const void* k, const void* v, in
 
 krpe_status_t krpe_attention_fwd_stats(const void* ws, size_t ws_bytes, int B, int H, int n, int d, int m,
                                        unsigned* fixed_rows, void* stream) {
-  g_last_error.clear();
+  clear_error();
   if (krpe_status_t s = check_dims(B, H, n, d, m, true, kMaxLongLog2N)) return s;
   if (!fixed_rows) return fail(KRPE_ERR_NULL, "fixed_rows must be non-NULL");
   *fixed_rows = 0;

@@ -1,0 +1,453 @@
+// Gradients of attention with a decaying bias (krpe_decay_bwd).  With the rows'
+// G_i = [g_i | gd_i] = [dz_i | -(dz_i . z_i)] / den_i, A the state before a
+// chunk and U the queries' sums phi(q_i) G_i^T after it:
+//
+//   dphi(q_i) = sum_{j <= i} e^{-rate (i - j)} (G_i . [v_j | 1]) phi(k_j) + e^{-rate (i + 1)} A^T G_i
+//   dphi(k_j) = sum_{i >= j} e^{-rate (i - j)} (G_i . [v_j | 1]) phi(q_i) + e^{-rate (C - j)} U^T [v_j | 1]
+//   dv_j      = sum_{i >= j} e^{-rate (i - j)} (phi(q_i) . phi(k_j)) g_i  + e^{-rate (C - j)} U phi(k_j)
+//   dx        = W^T (dphi o phi) - x sum(dphi o phi)   (through the row's norm when normalising)
+//
+// (i, j in the chunk of C rows.)  One kernel has both sides: the queries'
+// (SIDE 0) first sums its rows' numerators and denominators like the forward
+// pass and leaves G behind for the sums backwards in time and for the keys'
+// side (SIDE 1), whose first sums are dv.
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "decay.hpp"
+#include "decay_states.hpp"
+#include "launch.hpp"
+
+namespace krpe {
+
+// Rows p0 .. p0 + 127 as operands over their columns: f[tile][ks][term][64], lane: row, column
+// 16 ks + 8 (t / 4) + 4 lh + t % 4; zeros past `rows` rows and past d.
+template <typename T, int DK, int NT>
+__device__ __forceinline__ void stage_rows(const T* __restrict__ x, int p0, int rows, int d, uint4* __restrict__ f) {
+  for (int e = threadIdx.x; e < 128 * DK * 2; e += 256) {
+    const int half = e & 1, ks = (e >> 1) % DK, r = e / (2 * DK);
+    const T* __restrict__ row = x + static_cast<size_t>(p0 + min(r, rows - 1)) * d;
+    float u[4], w[4];
+    load4(row, 16 * ks + 4 * half, r < rows, d, u);
+    load4(row, 16 * ks + 4 * half + 8, r < rows, d, w);
+    uint32_t p[4][NT];
+    split_pair<NT>(u[0], u[1], p[0]), split_pair<NT>(u[2], u[3], p[1]);
+    split_pair<NT>(w[0], w[1], p[2]), split_pair<NT>(w[2], w[3], p[3]);
+#pragma unroll
+    for (int s = 0; s < NT; ++s)
+      f[(((r >> 5) * DK + ks) * NT + s) * kFragLanes + 32 * half + (r & 31)] = make_uint4(p[0][s], p[1][s], p[2][s], p[3][s]);
+  }
+}
+
+// Gradient of a lane's row (columns 32 t + 8 g + 4 lh + j along the registers) from
+// y = W^T p (elu + 1: p itself) and sum(p).
+template <typename TX, int DT, bool ELU>
+__device__ __forceinline__ void store_row_gradient(const TX* __restrict__ x, floatx16 (&y)[DT], float sum, TX* __restrict__ o,
+                                                   bool ok, int d, bool nprf) {
+  const int lh = (threadIdx.x & 63) >> 5;
+  float xv[DT][16];
+  float sq = 0.f;
+#pragma unroll
+  for (int t = 0; t < DT; ++t)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      float u[4];
+      load4(x, 32 * t + 8 * g + 4 * lh, true, d, u);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) xv[t][4 * g + j] = u[j], sq = fmaf(u[j], u[j], sq);
+    }
+  sq += __shfl_xor(sq, 32);
+  const float inv = nprf ? (sq > 0.f ? rsqrtf(sq) : 0.f) : 1.f;
+  float dot = 0.f;
+#pragma unroll
+  for (int t = 0; t < DT; ++t)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      xv[t][e] *= inv;
+      if constexpr (!ELU) y[t][e] = fmaf(-xv[t][e], sum, y[t][e]);
+      dot = fmaf(xv[t][e], y[t][e], dot);
+    }
+  dot += __shfl_xor(dot, 32);
+  if (!ok) return;
+#pragma unroll
+  for (int t = 0; t < DT; ++t)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      float u[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int e = 4 * g + j;
+        u[j] = nprf ? fmaf(-xv[t][e], dot, y[t][e]) * inv : y[t][e];
+      }
+      store4(o, 32 * t + 8 * g + 4 * lh, d, u);
+    }
+}
+
+template <typename TX, int DK, int NT, int SIDE, bool ELU>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k_decay_grad(DecayArgs a) {
+  using TG = typename std::conditional<SIDE == 0, TX, float>::type;  // values of the other rows: v, or g
+  constexpr int NSX = kTermsX<TX>, DT = DK / 2, NW = 3;
+  extern __shared__ __align__(16) uint4 smem[];
+  // first pass                                        second pass
+  uint4* const wl = smem;                           // wl   [DK][3][64]
+  uint4* const kl = wl + DK * NW * kFragLanes;      // kl   [4][2][NT][64]
+  uint4* const sl = kl + 8 * NT * kFragLanes;       // sl   [DT][2][NT][64]; then [DK][NT][64]
+  uint4* const tl = sl + DK * NT * kFragLanes;      // tl   [DT][2][NT][64]
+  uint4* const vl = smem;                           // between: columns [4][DT][2][NT][64], rows [4][DK][NT][64]
+  __shared__ __align__(16) float sden[32], sgd[kChunk];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lr = lane & 31, lh = lane >> 5;
+  const int ch = blockIdx.x % a.nchunk, bh = blockIdx.x / a.nchunk, b = bh / a.H, h = bh % a.H, d = a.d;
+  const int p0 = ch * kChunk, rows = rows_of(a.lens, b, a.n), cnt = min(kChunk, rows - p0);
+  if (cnt <= 0) return;
+  const size_t base = static_cast<size_t>(bh) * a.n * d, cells = static_cast<size_t>(d + 1) * a.Mp;
+  const float rl = rate_log2(a.rate[h]);
+  const float* __restrict__ W = a.W + static_cast<size_t>(h) * a.M * d;
+  const int seg = ch / a.segc, c0 = seg * a.segc, c1 = min(min(a.nchunk, c0 + a.segc), (rows + kChunk - 1) / kChunk);
+  const bool inner = SIDE == 0 ? ch > c0 : ch + 1 < c1;
+  const float* __restrict__ pre = inner ? (SIDE == 0 ? a.pre : a.preb) + (static_cast<size_t>(bh) * a.nchunk + ch) * cells : nullptr;
+  const float* __restrict__ old = (SIDE == 0 ? a.tot : a.totb) + (static_cast<size_t>(bh) * a.nseg + seg) * cells;
+  const float wold = decay(rl, SIDE == 0 ? (ch - c0) * kChunk : min(rows, c1 * kChunk) - (p0 + cnt));
+  const int i = 32 * wave + lr;  // the lane's own row
+  const float share = decay(rl, SIDE == 0 ? i + 1 : cnt - min(i, cnt));  // of the state outside the chunk
+  const size_t row = static_cast<size_t>(p0 + min(i, cnt - 1)) * d;
+  const TX* __restrict__ own = static_cast<const TX*>(SIDE == 0 ? a.q : a.k) + base + row;
+  const TX* __restrict__ oth = static_cast<const TX*>(SIDE == 0 ? a.k : a.q) + base + row;
+  const TG* __restrict__ vals = (SIDE == 0 ? static_cast<const TG*>(a.v) : reinterpret_cast<const TG*>(a.g)) + base;
+  auto uses = [&](int t) { return SIDE == 0 ? t <= wave : t >= wave; };  // tiles of the other rows
+  auto weight = [&](int t, int e) {
+    const int j = 32 * t + 8 * (e >> 2) + 4 * lh + (e & 3);
+    const int dist = SIDE == 0 ? i - j : j - i;
+    return dist >= 0 ? decay(rl, dist) : 0.f;
+  };
+  uint4 of[DK][NSX], tf[DK][NSX];
+  const RowFactors fo = row_factors<ELU>(load_x<TX, DK>(own, i < cnt, d, of), a.nprf, a.log2_m);
+  const RowFactors ft = row_factors<ELU>(load_x<TX, DK>(oth, i < cnt, d, tf), a.nprf, a.log2_m);
+  // [g | gd] of the lane's row (SIDE 0), or its values (SIDE 1)
+  floatx16 G[DT];
+  float gd = 1.f;
+  {
+    floatx16 S[4], Z[DT];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) S[t] = zero16();
+#pragma unroll
+    for (int t = 0; t < DT; ++t) Z[t] = zero16();
+    float den = 0.f;
+    for (int f0 = 0; f0 < a.Mp; f0 += 32) {
+      __syncthreads();
+      stage_weights<DK, NW, ELU>(W, f0, a.M, d, wl);
+      for (int e = threadIdx.x; e < DT * 32 * 4; e += 256) {
+        const int c = e >> 2, ks = (e >> 1) & 1, half = e & 1;
+        floatx16 x = zero16();  // (eight used)
+        if (c < d) {
+          const size_t at = static_cast<size_t>(c) * a.Mp + f0 + 16 * ks + 4 * half;
+#pragma unroll
+          for (int t = 0; t < 8; ++t) {
+            const size_t p = at + (t & 3) + 8 * (t >> 2);
+            x[t] = wold * old[p] + (pre ? pre[p] : 0.f);
+          }
+        }
+        uint4 t[NT];
+        pack_half<NT>(x, 0, t);
+#pragma unroll
+        for (int s = 0; s < NT; ++s) sl[(((c >> 5) * 2 + ks) * NT + s) * kFragLanes + 32 * half + (c & 31)] = t[s];
+      }
+      if (threadIdx.x < 32) {
+        const size_t at = static_cast<size_t>(d) * a.Mp + f0 + threadIdx.x;
+        sden[threadIdx.x] = wold * old[at] + (pre ? pre[at] : 0.f);
+      }
+      __syncthreads();
+      floatx16 acc, lo, ph;
+      const bool part = f0 + 32 > a.M;
+      project_terms<DK, NSX, NW, false>(wl, tf, acc, lo);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        ph[e] = feature<ELU>(acc[e], lo[e], ft.r, ft.c, ft.f);
+        if (part && f0 + 8 * (e >> 2) + 4 * lh + (e & 3) >= a.M) ph[e] = 0.f;
+      }
+#pragma unroll
+      for (int k2 = 0; k2 < 2; ++k2) {
+        uint4 t[NT];
+        pack_half<NT>(ph, k2, t);
+#pragma unroll
+        for (int s = 0; s < NT; ++s) kl[((wave * 2 + k2) * NT + s) * kFragLanes + lane] = t[s];
+      }
+      project_terms<DK, NSX, NW, false>(wl, of, acc, lo);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        ph[e] = feature<ELU>(acc[e], lo[e], fo.r, fo.c, fo.f);
+        if (part && f0 + 8 * (e >> 2) + 4 * lh + (e & 3) >= a.M) ph[e] = 0.f;
+      }
+      uint4 po[2][NT];
+      pack_half<NT>(ph, 0, po[0]);
+      pack_half<NT>(ph, 1, po[1]);
+      if constexpr (SIDE == 0) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) den = fmaf(sden[8 * (e >> 2) + 4 * lh + (e & 3)], ph[e], den);
+      }
+#pragma unroll
+      for (int ct = 0; ct < DT; ++ct)
+#pragma unroll
+        for (int k2 = 0; k2 < 2; ++k2) {
+          uint4 t[NT];
+          read_terms<NT>(sl + (ct * 2 + k2) * NT * kFragLanes, t);
+          Z[ct] = mfma_terms<NT, NT>(t, po[k2], Z[ct]);
+        }
+      __syncthreads();
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+        if (uses(t)) {
+#pragma unroll
+          for (int k2 = 0; k2 < 2; ++k2) {
+            uint4 f[NT];
+            read_terms<NT>(kl + (t * 2 + k2) * NT * kFragLanes, f);
+            S[t] = mfma_terms<NT, NT>(f, po[k2], S[t]);
+          }
+        }
+    }
+    den *= share;
+#pragma unroll
+    for (int ct = 0; ct < DT; ++ct)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) Z[ct][e] *= share;
+    __syncthreads();
+    stage_columns<TG, DT, NT, Values::kAsIs>(vals, p0, cnt, d, 4, vl, nullptr);
+    if (SIDE == 1 && threadIdx.x < kChunk)
+      sgd[threadIdx.x] = static_cast<int>(threadIdx.x) < cnt ? a.gd[static_cast<size_t>(bh) * a.n + p0 + threadIdx.x] : 0.f;
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+      if (uses(t)) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          S[t][e] *= weight(t, e);
+          if constexpr (SIDE == 0) den += S[t][e];
+        }
+#pragma unroll
+        for (int k2 = 0; k2 < 2; ++k2) {
+          uint4 pf[NT];
+          pack_half<NT>(S[t], k2, pf);
+#pragma unroll
+          for (int ct = 0; ct < DT; ++ct) {
+            uint4 f[NT];
+            read_terms<NT>(vl + ((t * DT + ct) * 2 + k2) * NT * kFragLanes, f);
+            Z[ct] = mfma_terms<NT, NT>(f, pf, Z[ct]);
+          }
+        }
+      }
+    if constexpr (SIDE == 0) {
+      den += __shfl_xor(den, 32);
+      const float inv = i < cnt ? 1.f / den : 0.f;
+      const TX* __restrict__ dz = static_cast<const TX*>(a.dz) + base + row;
+      float* __restrict__ g = a.g + base + row;
+      float dot = 0.f;
+#pragma unroll
+      for (int ct = 0; ct < DT; ++ct)
+#pragma unroll
+        for (int g4 = 0; g4 < 4; ++g4) {
+          const int c = 32 * ct + 8 * g4 + 4 * lh;
+          float u[4];
+          load4(dz, c, i < cnt, d, u);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            u[j] *= inv;
+            dot = fmaf(u[j], Z[ct][4 * g4 + j], dot);
+            G[ct][4 * g4 + j] = u[j];
+          }
+          if (i < cnt) store4(g, c, d, u);
+        }
+      gd = -(dot + __shfl_xor(dot, 32)) * inv;
+      if (i < cnt && lh == 0) a.gd[static_cast<size_t>(bh) * a.n + p0 + i] = gd;
+    } else {
+      const TX* __restrict__ v = static_cast<const TX*>(a.v) + base + row;
+      TX* __restrict__ dv = static_cast<TX*>(a.dv) + base + row;
+#pragma unroll
+      for (int ct = 0; ct < DT; ++ct)
+#pragma unroll
+        for (int g4 = 0; g4 < 4; ++g4) {
+          const int c = 32 * ct + 8 * g4 + 4 * lh;
+          float u[4];
+          load4(v, c, i < cnt, d, u);
+#pragma unroll
+          for (int j = 0; j < 4; ++j) G[ct][4 * g4 + j] = u[j];
+          const float o[4] = {Z[ct][4 * g4], Z[ct][4 * g4 + 1], Z[ct][4 * g4 + 2], Z[ct][4 * g4 + 3]};
+          if (i < cnt) store4(dv, c, d, o);
+        }
+    }
+  }
+  // R = e^{-rate (i - j)} (G_i . [v_j | 1]) as operands, and the lane's own values with the
+  // weight of the state outside the chunk
+  uint4 R[4][2][NT], gf[DT][2][NT];
+  __syncthreads();
+  stage_rows<TG, DK, NT>(vals, p0, cnt, d, vl);
+  __syncthreads();
+#pragma unroll
+  for (int ct = 0; ct < DT; ++ct)
+#pragma unroll
+    for (int k2 = 0; k2 < 2; ++k2) pack_half<NT>(G[ct], k2, gf[ct][k2]);
+#pragma unroll
+  for (int t = 0; t < 4; ++t)
+    if (uses(t)) {
+      floatx16 r = zero16();
+#pragma unroll
+      for (int ks = 0; ks < DK; ++ks) {
+        uint4 f[NT];
+        read_terms<NT>(vl + (t * DK + ks) * NT * kFragLanes, f);
+        r = mfma_terms<NT, NT>(f, gf[ks >> 1][ks & 1], r);
+      }
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float one = SIDE == 0 ? gd : sgd[32 * t + 8 * (e >> 2) + 4 * lh + (e & 3)];
+        r[e] = (r[e] + one) * weight(t, e);
+      }
+      pack_half<NT>(r, 0, R[t][0]);
+      pack_half<NT>(r, 1, R[t][1]);
+    }
+#pragma unroll
+  for (int ct = 0; ct < DT; ++ct) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) G[ct][e] *= share;
+#pragma unroll
+    for (int k2 = 0; k2 < 2; ++k2) pack_half<NT>(G[ct], k2, gf[ct][k2]);
+  }
+  const float one = gd * share;
+  floatx16 Y[DT];
+#pragma unroll
+  for (int t = 0; t < DT; ++t) Y[t] = zero16();
+  float psum = 0.f;
+  for (int f0 = 0; f0 < a.Mp; f0 += 32) {
+    __syncthreads();
+    stage_weights<DK, NW, ELU>(W, f0, a.M, d, wl);
+    // the state with rows l and the columns in the slots, and W with rows c and features in them
+    for (int e = threadIdx.x; e < 32 * DK * 2; e += 256) {
+      const int l = e & 31, half = (e >> 5) & 1, ks = e >> 6;
+      floatx16 x;
+#pragma unroll
+      for (int t = 0; t < 8; ++t) {
+        const int c = 16 * ks + 8 * (t >> 2) + 4 * half + (t & 3);
+        const size_t p = static_cast<size_t>(min(c, d)) * a.Mp + f0 + l;
+        x[t] = c < d ? wold * old[p] + (pre ? pre[p] : 0.f) : 0.f;
+      }
+      uint4 t[NT];
+      pack_half<NT>(x, 0, t);
+#pragma unroll
+      for (int s = 0; s < NT; ++s) sl[(ks * NT + s) * kFragLanes + 32 * half + l] = t[s];
+    }
+    for (int e = threadIdx.x; e < 32 * DT * 4; e += 256) {
+      const int c = e % (32 * DT), half = (e / (32 * DT)) & 1, k2 = e / (64 * DT);
+      floatx16 x;
+#pragma unroll
+      for (int t = 0; t < 8; ++t) {
+        const int l = f0 + 16 * k2 + 8 * (t >> 2) + 4 * half + (t & 3);
+        if constexpr (ELU)
+          x[t] = l == c ? 1.f : 0.f;
+        else
+          x[t] = l < a.M && c < d ? W[static_cast<size_t>(l) * d + c] : 0.f;
+      }
+      uint4 t[NT];
+      pack_half<NT>(x, 0, t);
+#pragma unroll
+      for (int s = 0; s < NT; ++s) tl[(((c >> 5) * 2 + k2) * NT + s) * kFragLanes + 32 * half + (c & 31)] = t[s];
+    }
+    if (threadIdx.x < 32) {
+      const size_t at = static_cast<size_t>(d) * a.Mp + f0 + threadIdx.x;
+      sden[threadIdx.x] = wold * old[at] + (pre ? pre[at] : 0.f);
+    }
+    __syncthreads();
+    floatx16 acc, lo, ph, df = zero16();
+    // features of the other rows with the positions along the registers: their factors by lane
+    project_terms<DK, NSX, NW, true>(wl, tf, acc, lo);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const int from = 8 * (e >> 2) + 4 * lh + (e & 3);  // the lane that holds this row's factors
+      ph[e] = feature<ELU>(acc[e], lo[e], __shfl(ft.r, from), __shfl(ft.c, from), __shfl(ft.f, from));
+    }
+    if (f0 + lr >= a.M) ph = zero16();
+#pragma unroll
+    for (int k2 = 0; k2 < 2; ++k2) {
+      uint4 t[NT];
+      pack_half<NT>(ph, k2, t);
+#pragma unroll
+      for (int s = 0; s < NT; ++s) kl[((wave * 2 + k2) * NT + s) * kFragLanes + lane] = t[s];
+    }
+#pragma unroll
+    for (int ks = 0; ks < DK; ++ks) {
+      uint4 f[NT];
+      read_terms<NT>(sl + ks * NT * kFragLanes, f);
+      df = mfma_terms<NT, NT>(f, gf[ks >> 1][ks & 1], df);
+    }
+    project_terms<DK, NSX, NW, false>(wl, of, acc, lo);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const int l = 8 * (e >> 2) + 4 * lh + (e & 3);
+      df[e] = fmaf(sden[l], one, df[e]);
+      ph[e] = feature<ELU>(acc[e], lo[e], fo.r, fo.c, fo.f);
+      if constexpr (ELU) ph[e] = fminf(ph[e], 1.f);  // the slope of elu + 1 is e^x below zero, 1 above
+      if (f0 + l >= a.M) ph[e] = 0.f;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int t = 0; t < 4; ++t)
+      if (uses(t)) {
+#pragma unroll
+        for (int k2 = 0; k2 < 2; ++k2) {
+          uint4 f[NT];
+          read_terms<NT>(kl + (t * 2 + k2) * NT * kFragLanes, f);
+          df = mfma_terms<NT, NT>(f, R[t][k2], df);
+        }
+      }
+#pragma unroll
+    for (int e = 0; e < 16; ++e) ph[e] *= df[e], psum += ph[e];
+#pragma unroll
+    for (int k2 = 0; k2 < 2; ++k2) {
+      uint4 pf[NT];
+      pack_half<NT>(ph, k2, pf);
+#pragma unroll
+      for (int ct = 0; ct < DT; ++ct) {
+        uint4 f[NT];
+        read_terms<NT>(tl + (ct * 2 + k2) * NT * kFragLanes, f);
+        Y[ct] = mfma_terms<NT, NT>(f, pf, Y[ct]);
+      }
+    }
+  }
+  psum += __shfl_xor(psum, 32);
+  TX* __restrict__ out = static_cast<TX*>(SIDE == 0 ? a.dq : a.dk) + base + row;
+  store_row_gradient<TX, DT, ELU>(own, Y, psum, out, i < cnt, d, a.nprf);
+}
+
+namespace {
+
+template <typename TX, int DK, bool ELU>
+hipError_t go(const DecayArgs& a, hipStream_t st) {
+  constexpr int NT = sizeof(TX) == 2 ? 2 : 3, NV = sizeof(TX) == 2 ? 1 : 3, DT = DK / 2;
+  constexpr int loop = DK * 3 + 8 * NT + DK * NT + DT * 2 * NT, mid = 4 * DK * NT;
+  constexpr int lds = (loop > mid ? loop : mid) * 1024;
+  if constexpr (lds > 65536) {
+    (void)hipFuncSetAttribute(reinterpret_cast<const void*>(&k_decay_grad<TX, DK, NT, 0, ELU>),
+                              hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    (void)hipFuncSetAttribute(reinterpret_cast<const void*>(&k_decay_grad<TX, DK, NT, 1, ELU>),
+                              hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  }
+  const dim3 grid(static_cast<unsigned>(a.B) * a.H * a.nchunk), block(256);
+  launch_decay_states<TX, TX, DK, NT, NV, ELU, false>(a, st);
+  hipLaunchKernelGGL((k_decay_grad<TX, DK, NT, 0, ELU>), grid, block, lds, st, a);
+  launch_decay_states<TX, float, DK, NT, NT, ELU, true>(a, st);
+  hipLaunchKernelGGL((k_decay_grad<TX, DK, NT, 1, ELU>), grid, block, lds, st, a);
+  return hipGetLastError();
+}
+template <typename TX, bool ELU>
+hipError_t by_width(const DecayArgs& a, hipStream_t st) {
+  if (a.d <= 32) return go<TX, 2, ELU>(a, st);
+  if (a.d <= 64) return go<TX, 4, ELU>(a, st);
+  return go<TX, 8, ELU>(a, st);
+}
+
+}  // namespace
+
+hipError_t launch_decay_bwd(bool bf16, bool elu, const DecayArgs& a, hipStream_t st) {
+  if (bf16) return elu ? by_width<uint16_t, true>(a, st) : by_width<uint16_t, false>(a, st);
+  return elu ? by_width<float, true>(a, st) : by_width<float, false>(a, st);
+}
+
+}  // namespace krpe

@@ -1,0 +1,243 @@
+// Prompts of attention with a decaying bias (krpe_decay_fwd): the state's sums
+// along each sequence, and the outputs of its chunks.
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+#include "decay.hpp"
+#include "decay_states.hpp"
+#include "launch.hpp"
+
+namespace krpe {
+
+// Outputs of a chunk.  A wave owns 32 rows (lane: row i), per 32 features:
+// its rows' phi(k) to LDS as fragments, phi(q) in registers; S^T[j][i] += phi(k)
+// phi(q) for the row tiles j up to its own and the numerators' share of the
+// state, A phi(q).  Then P = S e^{-rate (i - j)} leaves its registers as the
+// operand of sum_j v_j P_ij.
+// NT: terms of features and values; NP: of P and the state.
+template <typename TX, int DK, int NT, int NP, bool ELU>
+__global__ __launch_bounds__(256) void k_decay_out(DecayArgs a) {
+  constexpr int NSX = kTermsX<TX>, DT = DK / 2, NW = NT == 1 ? 2 : 3;
+  extern __shared__ __align__(16) uint4 smem[];
+  uint4* const wl = smem;                            // [DK][NW][64]
+  uint4* const sl = wl + DK * NW * kFragLanes;       // [DT][2][NP][64]
+  uint4* const kl = sl + DT * 2 * NP * kFragLanes;   // [4][2][NT][64]
+  uint4* const vl = smem;                            // [4][DT][2][NT][64], after the features
+  __shared__ __align__(16) float sden[32];
+  __shared__ int odd;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lr = lane & 31, lh = lane >> 5;
+  const int ch = blockIdx.x % a.nchunk, bh = blockIdx.x / a.nchunk, b = bh / a.H, h = bh % a.H, d = a.d;
+  const int p0 = ch * kChunk, rows = rows_of(a.lens, b, a.n), cnt = min(kChunk, rows - p0);
+  if (cnt <= 0) return;
+  const int slot = a.state ? slot_of(a.slots, b, a.B, a.nslots) : kStateNone;
+  const size_t base = static_cast<size_t>(bh) * a.n * d, cells = static_cast<size_t>(d + 1) * a.Mp;
+  const float rl = rate_log2(a.rate[h]);
+  const int seg = ch / a.segc, inseg = ch - seg * a.segc;
+  const float* __restrict__ pre = inseg ? a.pre + (static_cast<size_t>(bh) * a.nchunk + ch) * cells : nullptr;
+  const float* __restrict__ old = a.tot ? a.tot + (static_cast<size_t>(bh) * a.nseg + seg) * cells : nullptr;
+  const float wold = decay(rl, inseg * kChunk);
+  const int i = 32 * wave + lr;
+  const size_t row = static_cast<size_t>(p0 + min(i, cnt - 1)) * d;
+  uint4 qf[DK][NSX], kf[DK][NSX];
+  const RowFactors fq = row_factors<ELU>(load_x<TX, DK>(static_cast<const TX*>(a.q) + base + row, i < cnt, d, qf), a.nprf,
+                                         a.log2_m);
+  const RowFactors fk = row_factors<ELU>(load_x<TX, DK>(static_cast<const TX*>(a.k) + base + row, i < cnt, d, kf), a.nprf,
+                                         a.log2_m);
+  floatx16 S[4], Z[DT];
+#pragma unroll
+  for (int t = 0; t < 4; ++t) S[t] = zero16();
+#pragma unroll
+  for (int t = 0; t < DT; ++t) Z[t] = zero16();
+  float den = 0.f;
+  if (threadIdx.x == 0) odd = 0;
+  for (int f0 = 0; f0 < a.Mp; f0 += 32) {
+    __syncthreads();  // the previous features consumed
+    stage_weights<DK, NW, ELU>(a.W + static_cast<size_t>(h) * a.M * d, f0, a.M, d, wl);
+    if (old) {
+      // the state before the chunk as operands: rows c, features in the slots' order
+      for (int e = threadIdx.x; e < DT * 32 * 4; e += 256) {
+        const int c = e >> 2, ks = (e >> 1) & 1, half = e & 1;
+        floatx16 x = zero16();  // (eight used)
+        if (c < d) {
+          const size_t at = static_cast<size_t>(c) * a.Mp + f0 + 16 * ks + 4 * half;
+          const float4 u = *reinterpret_cast<const float4*>(old + at), w = *reinterpret_cast<const float4*>(old + at + 8);
+          x[0] = wold * u.x, x[1] = wold * u.y, x[2] = wold * u.z, x[3] = wold * u.w;
+          x[4] = wold * w.x, x[5] = wold * w.y, x[6] = wold * w.z, x[7] = wold * w.w;
+          if (pre) {
+            const float4 y = *reinterpret_cast<const float4*>(pre + at), t = *reinterpret_cast<const float4*>(pre + at + 8);
+            x[0] += y.x, x[1] += y.y, x[2] += y.z, x[3] += y.w;
+            x[4] += t.x, x[5] += t.y, x[6] += t.z, x[7] += t.w;
+          }
+        }
+        uint4 t[NP];
+        pack_half<NP>(x, 0, t);
+#pragma unroll
+        for (int s = 0; s < NP; ++s) sl[(((c >> 5) * 2 + ks) * NP + s) * kFragLanes + 32 * half + (c & 31)] = t[s];
+      }
+      if (threadIdx.x < 32) {
+        const size_t at = static_cast<size_t>(d) * a.Mp + f0 + threadIdx.x;
+        sden[threadIdx.x] = wold * old[at] + (pre ? pre[at] : 0.f);
+      }
+    }
+    __syncthreads();
+    floatx16 acc, lo, ph;
+    project_terms<DK, NSX, NW, false>(wl, kf, acc, lo);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) ph[e] = feature<ELU>(acc[e], lo[e], fk.r, fk.c, fk.f);
+    const bool part = f0 + 32 > a.M;  // uniform: features past M weigh nothing
+    if (part) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (f0 + 8 * (e >> 2) + 4 * lh + (e & 3) >= a.M) ph[e] = 0.f;
+    }
+#pragma unroll
+    for (int k2 = 0; k2 < 2; ++k2) {
+      uint4 t[NT];
+      pack_half<NT>(ph, k2, t);
+#pragma unroll
+      for (int s = 0; s < NT; ++s) kl[((wave * 2 + k2) * NT + s) * kFragLanes + lane] = t[s];
+    }
+    project_terms<DK, NSX, NW, false>(wl, qf, acc, lo);
+#pragma unroll
+    for (int e = 0; e < 16; ++e) ph[e] = feature<ELU>(acc[e], lo[e], fq.r, fq.c, fq.f);
+    if (part) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e)
+        if (f0 + 8 * (e >> 2) + 4 * lh + (e & 3) >= a.M) ph[e] = 0.f;
+    }
+    uint4 pq[2][NT];
+    pack_half<NT>(ph, 0, pq[0]);
+    pack_half<NT>(ph, 1, pq[1]);
+    if (old) {
+#pragma unroll
+      for (int g = 0; g < 4; ++g) {
+        const float4 s4 = *reinterpret_cast<const float4*>(sden + 8 * g + 4 * lh);
+        den = fmaf(s4.x, ph[4 * g], den), den = fmaf(s4.y, ph[4 * g + 1], den);
+        den = fmaf(s4.z, ph[4 * g + 2], den), den = fmaf(s4.w, ph[4 * g + 3], den);
+      }
+#pragma unroll
+      for (int ct = 0; ct < DT; ++ct)
+#pragma unroll
+        for (int k2 = 0; k2 < 2; ++k2) {
+          uint4 t[NP];
+          read_terms<NP>(sl + (ct * 2 + k2) * NP * kFragLanes, t);
+          Z[ct] = mfma_terms<NP, NT>(t, pq[k2], Z[ct]);
+        }
+    }
+    __syncthreads();  // phi(k) of all rows
+#pragma unroll
+    for (int jt = 0; jt < 4; ++jt)
+      if (jt <= wave) {
+#pragma unroll
+        for (int k2 = 0; k2 < 2; ++k2) {
+          uint4 t[NT];
+          read_terms<NT>(kl + (jt * 2 + k2) * NT * kFragLanes, t);
+          S[jt] = mfma_terms<NT, NT>(t, pq[k2], S[jt]);
+        }
+      }
+  }
+  // the state's share reaches row i over i + 1 positions
+  const float since = decay(rl, i + 1);
+  den *= since;
+#pragma unroll
+  for (int ct = 0; ct < DT; ++ct)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) Z[ct][e] *= since;
+  const TX* __restrict__ v = static_cast<const TX*>(a.v) + base;
+  __syncthreads();
+  stage_columns<TX, DT, NT, Values::kClean>(v, p0, cnt, d, 4, vl, &odd);
+  __syncthreads();
+#pragma unroll
+  for (int jt = 0; jt < 4; ++jt)
+    if (jt <= wave) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int dist = i - (32 * jt + 8 * (e >> 2) + 4 * lh + (e & 3));
+        S[jt][e] = dist >= 0 ? S[jt][e] * decay(rl, dist) : 0.f;
+        den += S[jt][e];
+      }
+#pragma unroll
+      for (int k2 = 0; k2 < 2; ++k2) {
+        uint4 pf[NP];
+        pack_half<NP>(S[jt], k2, pf);
+#pragma unroll
+        for (int ct = 0; ct < DT; ++ct) {
+          uint4 t[NT];
+          read_terms<NT>(vl + ((jt * DT + ct) * 2 + k2) * NT * kFragLanes, t);
+          Z[ct] = mfma_terms<NT, NP>(t, pf, Z[ct]);
+        }
+      }
+    }
+  den += __shfl_xor(den, 32);
+  if (odd) {
+    // values that are not finite (they went in as zeros): NaN for the rows that see them.
+    // The same product over marks, 1 for such a value and 1 for a position that is seen.
+    __syncthreads();
+    stage_columns<TX, DT, 1, Values::kMark>(v, p0, cnt, d, 4, vl, nullptr);
+    __syncthreads();
+    for (int jt = 0; jt <= wave; ++jt)
+#pragma unroll
+      for (int k2 = 0; k2 < 2; ++k2) {
+        floatx16 seen;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) seen[e] = i >= 32 * jt + 8 * (e >> 2) + 4 * lh + (e & 3) ? 1.f : 0.f;
+        uint4 pf[1];
+        pack_half<1>(seen, k2, pf);
+#pragma unroll
+        for (int ct = 0; ct < DT; ++ct) {
+          uint4 t[1];
+          read_terms<1>(vl + ((jt * DT + ct) * 2 + k2) * kFragLanes, t);
+          const floatx16 marks = mfma_bf16(t[0], pf[0], zero16());
+#pragma unroll
+          for (int e = 0; e < 16; ++e) Z[ct][e] = marks[e] > 0.f ? NAN : Z[ct][e];
+        }
+      }
+  }
+  if (i >= cnt) return;
+  using TZ = TX;
+  TZ* __restrict__ z = static_cast<TZ*>(a.z) + base + row;
+  const float inv = slot == kStateBad ? NAN : 1.f / den;
+#pragma unroll
+  for (int ct = 0; ct < DT; ++ct)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const float o[4] = {Z[ct][4 * g] * inv, Z[ct][4 * g + 1] * inv, Z[ct][4 * g + 2] * inv, Z[ct][4 * g + 3] * inv};
+      store4(z, 32 * ct + 8 * g + 4 * lh, d, o);
+    }
+}
+
+namespace {
+
+template <typename TX, int DK, bool ELU>
+hipError_t go(const DecayArgs& a, hipStream_t st) {
+  constexpr int NT = sizeof(TX) == 2 ? 1 : 3, NP = sizeof(TX) == 2 ? 2 : 3, DT = DK / 2;
+  const int BH = a.B * a.H;
+  if (a.tot) launch_decay_states<TX, TX, DK, 3, NT, ELU, false>(a, st);
+  if (a.nchunk > 0) {
+    constexpr int NW = NT == 1 ? 2 : 3;
+    constexpr int feat = DK * NW + DT * 2 * NP + 8 * NT, vals = 8 * DT * NT;
+    constexpr int lds = (feat > vals ? feat : vals) * 1024;
+    if constexpr (lds > 65536)
+      (void)hipFuncSetAttribute(reinterpret_cast<const void*>(&k_decay_out<TX, DK, NT, NP, ELU>),
+                                hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+    hipLaunchKernelGGL((k_decay_out<TX, DK, NT, NP, ELU>), dim3(static_cast<unsigned>(BH) * a.nchunk), dim3(256), lds, st, a);
+  }
+  return hipGetLastError();
+}
+template <typename TX, bool ELU>
+hipError_t by_width(const DecayArgs& a, hipStream_t st) {
+  if (a.d <= 32) return go<TX, 2, ELU>(a, st);
+  if (a.d <= 64) return go<TX, 4, ELU>(a, st);
+  return go<TX, 8, ELU>(a, st);
+}
+
+}  // namespace
+
+hipError_t launch_decay_fwd(bool bf16, bool elu, const DecayArgs& a, hipStream_t st) {
+  if (bf16) return elu ? by_width<uint16_t, true>(a, st) : by_width<uint16_t, false>(a, st);
+  return elu ? by_width<float, true>(a, st) : by_width<float, false>(a, st);
+}
+
+}  // namespace krpe

@@ -9,6 +9,12 @@ any of these without the built library or without a GPU raises.
 Names and layouts follow the C header ``include/krpe.h``:
   q, k, v : [B, H, n, d]  float32 or bfloat16      W : [H, m, d] float32
   b       : [H, 2n-1] float32, b[h, s] = b_{s-(n-1)} (Algorithm 1's ordering)
+
+The decay_* functions are Eq. (10) with the bias b_t = rate t (t <= 0, -inf after)
+over a state of constant size: prompts, their gradients, single tokens, trees of
+drafted tokens, and copies within a pool of states.  Their outputs have q's type.
+  rate    : [H] float32         state : [slots, H, d + 1, M] float32, changed in place
+  slots   : [B] int32, the pool's row of each sequence (None: row b; -1: none)
 """
 from __future__ import annotations
 
@@ -21,7 +27,9 @@ __all__ = ["KrpeError", "load", "lib_path", "feature_map", "toeplitz_conv", "toe
            "attention_fwd", "attention_bwd",
            "attention_fwd_route",
            "attention_fwd_workspace", "attention_bwd_workspace", "toeplitz_conv_workspace",
-           "attention_fwd_fixed_rows", "DTYPES"]
+           "attention_fwd_fixed_rows", "decay_state", "decay_attention_fwd", "decay_attention_bwd",
+           "decay_attention_step", "decay_attention_tree", "decay_attention_commit", "decay_state_copy",
+           "decay_attention_fwd_workspace", "decay_attention_bwd_workspace", "DTYPES"]
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 _LIB_PATH = os.path.join(_HERE, "libkrpe.so")
@@ -37,6 +45,8 @@ ROUTE_DIRECT = 8  # option bit: evaluate Eq. (10) directly (quadratic, MFMA)
 ROUTE_FFT = 16  # option bit: the FFT route of Section 3.2
 ROUTES = {"auto": 0, "direct": ROUTE_DIRECT, "fft": ROUTE_FFT}
 HINT_CAUSAL = 32  # option bit: b is -inf for every t > 0 (read by the route choice only)
+STATE_FRESH = 64  # option bit of decay_attention_fwd: sequences start from zeros
+TREE_MAX, COPY_MAX = 64, 256  # nodes of a tree, moves of a copy
 
 
 class KrpeError(RuntimeError):
@@ -95,6 +105,18 @@ def load(path: str | None = None) -> ctypes.CDLL:
                                        sz, vp]
     lib.krpe_attention_fwd_stats.restype = i
     lib.krpe_attention_fwd_stats.argtypes = [vp, sz, i, i, i, i, i, ctypes.POINTER(ctypes.c_uint), vp]
+    u = ctypes.c_uint
+    for name, res, args in (
+            ("krpe_decay_fwd_workspace", sz, [i, i, i, i, i, u]),
+            ("krpe_decay_fwd", i, [vp, vp, vp, i, vp, vp, vp, vp, vp, i, vp, i, i, i, i, i, u, vp, sz, vp]),
+            ("krpe_decay_bwd_workspace", sz, [i, i, i, i, i, u]),
+            ("krpe_decay_bwd", i, [vp, vp, vp, i, vp, vp, vp, vp, vp, vp, vp, i, i, i, i, i, u, vp, sz, vp]),
+            ("krpe_decay_step", i, [vp, vp, vp, i, vp, vp, vp, vp, vp, i, i, i, i, i, u, vp]),
+            ("krpe_decay_tree", i, [vp, vp, vp, i, vp, vp, vp, vp, vp, vp, i, i, i, i, i, i, u, vp]),
+            ("krpe_decay_commit", i, [vp, vp, i, vp, vp, vp, vp, vp, i, i, i, i, i, i, i, u, vp]),
+            ("krpe_decay_state_copy", i, [vp, vp, vp, i, i, i, i, i, vp])):
+        getattr(lib, name).restype = res
+        getattr(lib, name).argtypes = args
     if path is None:
         _lib = lib
     return lib
@@ -332,3 +354,219 @@ def attention_bwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, b: torch.Te
                                 workspace.numel(), _stream(q.device))
     _check(st, "krpe_attention_bwd")
     return (dq, dk, dv, db) if with_db else (dq, dk, dv)
+
+
+# ---- attention with a decaying bias -------------------------------------------------
+
+def _decay_flags(nprf: bool, features: str) -> int:
+    if features not in ("prf", "elu"):
+        raise KrpeError(f"features must be one of ['elu', 'prf'] here, got {features!r}")
+    return (NPRF if nprf else 0) | FEATURES[features]
+
+
+def _enqueue(name: str, device: torch.device, *args) -> None:
+    """The C call `name` on the current stream of `device`, with that device the current one."""
+    fn = getattr(load(), name)
+    if torch.cuda.current_device() == device.index:
+        _check(fn(*args, _stream(device)), name)
+    else:
+        with torch.cuda.device(device):
+            _check(fn(*args, _stream(device)), name)
+
+
+def _decay_inputs(tensors: dict, rate: torch.Tensor, W: torch.Tensor | None, features: str, dims: int):
+    """Checked, contiguous inputs of one shape [B, H, (rows,) d] and type; rate, W and m."""
+    out = []
+    first = None
+    for name, t in tensors.items():
+        t = _gpu(t, name)
+        if first is None:
+            first = t
+            if t.dim() != dims:
+                raise KrpeError(f"{name} must have {dims} dimensions")
+        elif t.shape != first.shape or t.dtype != first.dtype:
+            raise KrpeError(f"{', '.join(tensors)} must share shape and dtype")
+        out.append(t)
+    _dtype_code(first, next(iter(tensors)))
+    H, d = first.shape[1], first.shape[-1]
+    rate = _gpu(rate, "rate")
+    if rate.shape != (H,) or rate.dtype != torch.float32:
+        raise KrpeError("rate must be float32 [H]")
+    W, m = _proj(W, H, d, features)
+    _one_device(first.device, *out[1:], rate, W)
+    return out, rate, W, m
+
+
+def _one_device(device: torch.device, *tensors) -> None:
+    for t in tensors:
+        if t is not None and t.device != device:
+            raise KrpeError(f"all tensors must be on one GPU: {t.device} and {device}")
+
+
+def _ints(t: torch.Tensor | None, name: str, shape: tuple, device: torch.device) -> torch.Tensor | None:
+    if t is None:
+        return None
+    t = _gpu(t, name)
+    if t.dtype != torch.int32 or tuple(t.shape) != shape:
+        raise KrpeError(f"{name} must be int32 {list(shape)}")
+    _one_device(device, t)
+    return t
+
+
+def _pool(state: torch.Tensor, H: int, d: int, m: int, device: torch.device) -> int:
+    """The number of slots of a pool, which has to be contiguous (it is changed in place)."""
+    if not isinstance(state, torch.Tensor) or not state.is_cuda:
+        raise KrpeError("state must be on a GPU (libkrpe has no CPU path)")
+    if state.dim() != 4 or state.shape[1:] != (H, d + 1, m) or state.dtype != torch.float32:
+        raise KrpeError(f"state must be float32 [slots, {H}, {d + 1}, {m}]")
+    if not state.is_contiguous():
+        raise KrpeError("state must be contiguous")
+    _one_device(device, state)
+    return state.shape[0]
+
+
+def _like(out: torch.Tensor | None, x: torch.Tensor, zeros: bool) -> torch.Tensor:
+    """The output beside input x: the one given, checked, or a new one."""
+    if out is None:
+        return torch.zeros_like(x) if zeros else torch.empty_like(x)
+    if not isinstance(out, torch.Tensor) or out.shape != x.shape or out.dtype != x.dtype or not out.is_contiguous():
+        raise KrpeError("out must be a contiguous tensor of q's shape and dtype")
+    _one_device(x.device, out)
+    return out
+
+
+def _space(workspace: torch.Tensor | None, need: int, device: torch.device) -> torch.Tensor:
+    if workspace is None:
+        return torch.empty(max(need, 1), dtype=torch.uint8, device=device)
+    if workspace.dtype != torch.uint8 or workspace.numel() < need or not workspace.is_contiguous():
+        raise KrpeError(f"workspace must hold at least {need} bytes (uint8)")
+    _one_device(device, workspace)
+    return workspace
+
+
+def decay_state(slots: int, H: int, d: int, m: int, device="cuda") -> torch.Tensor:
+    """A pool of empty states [slots, H, d + 1, m] (m: the features; d with features="elu")."""
+    return torch.zeros((slots, H, d + 1, m), dtype=torch.float32, device=device)
+
+
+def decay_attention_fwd_workspace(B: int, H: int, n: int, d: int, m: int) -> int:
+    return int(load().krpe_decay_fwd_workspace(B, H, n, d, m, 0))
+
+
+def decay_attention_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, rate: torch.Tensor, W: torch.Tensor | None,
+                        state: torch.Tensor | None = None, slots: torch.Tensor | None = None,
+                        lens: torch.Tensor | None = None, fresh: bool = False, out: torch.Tensor | None = None,
+                        workspace: torch.Tensor | None = None, nprf: bool = False,
+                        features: str = "prf") -> torch.Tensor:
+    """Eq. (10) with b_t = rate t (t <= 0): z [B,H,n,d] in q's type, O(n).
+
+    ``state``: the pool whose rows are the states before the sequences (zeros with
+    ``fresh``, whatever the rows hold) and, after the call, those behind them.
+    ``lens``: int32 [B], the positions of each sequence; rows of q, k, v behind them are
+    not read and rows of ``out`` stay as they were (zeros without ``out``)."""
+    flags = _decay_flags(nprf, features)
+    (q, k, v), rate, W, m = _decay_inputs({"q": q, "k": k, "v": v}, rate, W, features, 4)
+    B, H, n, d = q.shape
+    dev = q.device
+    nslots = 0
+    if state is not None:
+        nslots = _pool(state, H, d, m, dev)
+        flags |= STATE_FRESH if fresh else 0
+    elif slots is not None or fresh:
+        raise KrpeError("slots and fresh need a state")
+    slots, lens = _ints(slots, "slots", (B,), dev), _ints(lens, "lens", (B,), dev)
+    z = _like(out, q, lens is not None)
+    ws = _space(workspace, int(load().krpe_decay_fwd_workspace(B, H, n, d, m, flags)), dev)
+    _enqueue("krpe_decay_fwd", dev, _ptr(q), _ptr(k), _ptr(v), DTYPES[q.dtype], _ptr(rate), _ptr(W), _ptr(z),
+             _ptr(state), _ptr(slots), nslots, _ptr(lens), B, H, n, d, m, flags, ws.data_ptr(), ws.numel())
+    return z
+
+
+def decay_attention_bwd_workspace(B: int, H: int, n: int, d: int, m: int) -> int:
+    return int(load().krpe_decay_bwd_workspace(B, H, n, d, m, 0))
+
+
+def decay_attention_bwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, rate: torch.Tensor, W: torch.Tensor | None,
+                        dz: torch.Tensor, lens: torch.Tensor | None = None, workspace: torch.Tensor | None = None,
+                        nprf: bool = False, features: str = "prf") -> tuple:
+    """Gradients (dq, dk, dv) [B,H,n,d] in q's type of sum(dz * z), z = decay_attention_fwd(q, k, v, rate, W)
+    from empty states, rate and W fixed.  Rows behind ``lens`` are zero."""
+    flags = _decay_flags(nprf, features)
+    (q, k, v, dz), rate, W, m = _decay_inputs({"q": q, "k": k, "v": v, "dz": dz}, rate, W, features, 4)
+    B, H, n, d = q.shape
+    lens = _ints(lens, "lens", (B,), q.device)
+    dq, dk, dv = (_like(None, q, lens is not None) for _ in range(3))
+    ws = _space(workspace, int(load().krpe_decay_bwd_workspace(B, H, n, d, m, flags)), q.device)
+    _enqueue("krpe_decay_bwd", q.device, _ptr(q), _ptr(k), _ptr(v), DTYPES[q.dtype], _ptr(rate), _ptr(W), _ptr(dz),
+             _ptr(dq), _ptr(dk), _ptr(dv), _ptr(lens), B, H, n, d, m, flags, ws.data_ptr(), ws.numel())
+    return dq, dk, dv
+
+
+def decay_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, rate: torch.Tensor, W: torch.Tensor | None,
+                         state: torch.Tensor, slots: torch.Tensor | None = None, out: torch.Tensor | None = None,
+                         nprf: bool = False, features: str = "prf") -> torch.Tensor:
+    """One token of every sequence: its k, v [B,H,d] go into the states, z [B,H,d] is its output.
+    Allocates nothing with ``out`` (a captured graph may replay it)."""
+    flags = _decay_flags(nprf, features)
+    (q, k, v), rate, W, m = _decay_inputs({"q": q, "k": k, "v": v}, rate, W, features, 3)
+    B, H, d = q.shape
+    nslots = _pool(state, H, d, m, q.device)
+    slots = _ints(slots, "slots", (B,), q.device)
+    z = _like(out, q, False)
+    _enqueue("krpe_decay_step", q.device, _ptr(q), _ptr(k), _ptr(v), DTYPES[q.dtype], _ptr(rate), _ptr(W), _ptr(z),
+             _ptr(state), _ptr(slots), nslots, B, H, d, m, flags)
+    return z
+
+
+def decay_attention_tree(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, parent: torch.Tensor, rate: torch.Tensor,
+                         W: torch.Tensor | None, state: torch.Tensor, slots: torch.Tensor | None = None,
+                         out: torch.Tensor | None = None, nprf: bool = False, features: str = "prf") -> torch.Tensor:
+    """Trees of drafted tokens q, k, v [B,H,T,d] (T <= 64) behind every sequence: z of each node from
+    the state, its ancestors and itself.  ``parent``: int32 [B,T], parent[b,t] < t, -1 for the children
+    of the sequence's last token; a node with any other parent, and what is below it, gets zeros.
+    The states stay as they are: decay_attention_commit takes the accepted nodes in."""
+    flags = _decay_flags(nprf, features)
+    (q, k, v), rate, W, m = _decay_inputs({"q": q, "k": k, "v": v}, rate, W, features, 4)
+    B, H, T, d = q.shape
+    nslots = _pool(state, H, d, m, q.device)
+    if parent is None:
+        raise KrpeError("parent must be int32 [B, T]")
+    parent, slots = _ints(parent, "parent", (B, T), q.device), _ints(slots, "slots", (B,), q.device)
+    z = _like(out, q, False)
+    _enqueue("krpe_decay_tree", q.device, _ptr(q), _ptr(k), _ptr(v), DTYPES[q.dtype], _ptr(parent), _ptr(rate), _ptr(W),
+             _ptr(z), _ptr(state), _ptr(slots), nslots, B, H, T, d, m, flags)
+    return z
+
+
+def decay_attention_commit(k: torch.Tensor, v: torch.Tensor, path: torch.Tensor, rate: torch.Tensor,
+                           W: torch.Tensor | None, state: torch.Tensor, slots: torch.Tensor | None = None,
+                           nprf: bool = False, features: str = "prf") -> None:
+    """Takes tokens path[b, 0], path[b, 1], .. of k, v [B,H,T,d] into the states, up to the first entry
+    outside [0, T).  ``path``: int32 [B,P]."""
+    flags = _decay_flags(nprf, features)
+    (k, v), rate, W, m = _decay_inputs({"k": k, "v": v}, rate, W, features, 4)
+    B, H, T, d = k.shape
+    nslots = _pool(state, H, d, m, k.device)
+    if not isinstance(path, torch.Tensor) or path.dim() != 2:
+        raise KrpeError("path must be int32 [B, P]")
+    path = _ints(path, "path", (B, path.shape[1]), k.device)
+    slots = _ints(slots, "slots", (B,), k.device)
+    _enqueue("krpe_decay_commit", k.device, _ptr(k), _ptr(v), DTYPES[k.dtype], _ptr(path), _ptr(rate), _ptr(W),
+             _ptr(state), _ptr(slots), nslots, B, H, T, path.shape[1], d, m, flags)
+
+
+def decay_state_copy(state: torch.Tensor, src: torch.Tensor, dst: torch.Tensor) -> None:
+    """state[dst[i]] = state[src[i]] for all i at once (src -1: cleared): forks, reorders, compacts and
+    frees the states of a pool.  ``src``, ``dst``: int32 [count], count <= 256.  Of moves to one slot the
+    last holds; moves with a slot outside the pool are left out."""
+    if not isinstance(state, torch.Tensor) or state.dim() != 4:
+        raise KrpeError("state must be float32 [slots, H, d + 1, m]")
+    nslots, H, rows, m = state.shape
+    _pool(state, H, rows - 1, m, state.device)
+    if not isinstance(src, torch.Tensor) or src.dim() != 1:
+        raise KrpeError("src must be int32 [count]")
+    src, dst = _ints(src, "src", (src.shape[0],), state.device), _ints(dst, "dst", (src.shape[0],), state.device)
+    if dst is None:
+        raise KrpeError("dst must be int32 [count]")
+    _enqueue("krpe_decay_state_copy", state.device, _ptr(state), _ptr(src), _ptr(dst), src.shape[0], nslots, H, rows - 1,
+             m)
