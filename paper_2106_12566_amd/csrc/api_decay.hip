@@ -9,7 +9,6 @@
 #include "api_util.hpp"
 #include "decay.hpp"
 #include "krpe.h"
-#include "launch.hpp"
 
 namespace krpe {
 namespace {

@@ -301,4 +301,13 @@ __device__ __forceinline__ int rows_of(const int* __restrict__ lens, int b, int 
   return lens ? min(max(lens[b], 0), n) : n;
 }
 
+// Host-side launchers (decay_fwd.hip, decay_bwd.hip, decay_step.hip, decay_tree.hip).
+hipError_t launch_decay_fwd(bool bf16, bool elu, const DecayArgs& a, hipStream_t st);
+hipError_t launch_decay_bwd(bool bf16, bool elu, const DecayArgs& a, hipStream_t st);
+hipError_t launch_decay_step(bool bf16, bool elu, const PoolArgs& a, hipStream_t st);
+hipError_t launch_decay_tree(bool bf16, bool elu, const PoolArgs& a, hipStream_t st);
+hipError_t launch_decay_commit(bool bf16, bool elu, const PoolArgs& a, hipStream_t st);
+hipError_t launch_state_copy(float* state, const int* src, const int* dst, int count, int nslots, long long cells,
+                             hipStream_t st);
+
 }  // namespace krpe

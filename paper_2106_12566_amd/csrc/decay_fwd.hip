@@ -6,7 +6,6 @@
 
 #include "decay.hpp"
 #include "decay_states.hpp"
-#include "launch.hpp"
 
 namespace krpe {
 

@@ -6,7 +6,6 @@
 #include <cstdint>
 
 #include "decay.hpp"
-#include "launch.hpp"
 
 namespace krpe {
 

@@ -14,7 +14,6 @@
 #include <cstdint>
 
 #include "decay.hpp"
-#include "launch.hpp"
 
 namespace krpe {
 

@@ -277,15 +277,4 @@ hipError_t launch_feature_bwd(bool bf16, const void* x, const float* W, const fl
 // y[bh][c][i] (row stride ldy) = sum over s of part[bh][s][c][i], i < n.
 hipError_t launch_sum_splits(const float* part, float* y, int BH, int C, int n, int ldy, int nsplit, hipStream_t st);
 
-// Attention with a decaying bias (decay.hpp): DecayArgs and PoolArgs are its kernels'.
-struct DecayArgs;
-struct PoolArgs;
-hipError_t launch_decay_fwd(bool bf16, bool elu, const DecayArgs& a, hipStream_t st);
-hipError_t launch_decay_bwd(bool bf16, bool elu, const DecayArgs& a, hipStream_t st);
-hipError_t launch_decay_step(bool bf16, bool elu, const PoolArgs& a, hipStream_t st);
-hipError_t launch_decay_tree(bool bf16, bool elu, const PoolArgs& a, hipStream_t st);
-hipError_t launch_decay_commit(bool bf16, bool elu, const PoolArgs& a, hipStream_t st);
-hipError_t launch_state_copy(float* state, const int* src, const int* dst, int count, int nslots, long long cells,
-                             hipStream_t st);
-
 }  // namespace krpe
