@@ -390,7 +390,7 @@ krpe_status_t krpe_decay_tree(const void* q, const void* k, const void* v, int q
 
 /*
  * Takes tokens path[b][0], path[b][1], .. of k, v [B, H, T, d] into the states, in that order, up
- * to the first entry outside [0, T) or P entries.  path: [B, P] int32 (device).
+ * to the first entry outside [0, T) or P entries; T <= 65536.  path: [B, P] int32 (device).
  */
 krpe_status_t krpe_decay_commit(const void* k, const void* v, int qkv_dtype, const int* path, const float* rate,
                                 const float* W, float* state, const int* slots, int nslots, int B, int H, int T,

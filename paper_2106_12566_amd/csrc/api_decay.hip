@@ -151,8 +151,7 @@ krpe_status_t krpe_decay_fwd(const void* q, const void* k, const void* v, int qk
   char* w = static_cast<char*>(ws);
   DecayArgs a{};
   a.q = q, a.k = k, a.v = v, a.z = z, a.rate = rate, a.W = W, a.state = state, a.slots = slots, a.lens = lens;
-  // (a single chunk from zeros whose state is not asked for needs no sums)
-  a.tot = state || L.nchunk > 1 ? reinterpret_cast<float*>(w + L.tot) : nullptr;
+  a.tot = reinterpret_cast<float*>(w + L.tot);
   a.pre = reinterpret_cast<float*>(w + L.pre);
   a.B = B, a.H = H, a.n = n, a.d = d, a.M = m, a.Mp = L.Mp, a.nchunk = L.nchunk, a.nseg = L.nseg, a.segc = L.segc;
   a.nslots = nslots, a.nprf = (flags & KRPE_NPRF) != 0, a.fresh = (flags & KRPE_STATE_FRESH) != 0;
@@ -246,7 +245,7 @@ krpe_status_t krpe_decay_tree(const void* q, const void* k, const void* v, int q
   for (const Range& r : ins)
     if (overlaps({z, x}, r)) return fail(KRPE_ERR_ALIAS, "z overlaps an input or the states");
   PoolArgs a = pool_args(q, k, v, z, rate, W, const_cast<float*>(state), slots, nslots, B, H, d, m, flags);
-  a.tree = parent, a.T = T;
+  a.parent = parent, a.T = T;
   return hip_check(launch_decay_tree(qkv_dtype == KRPE_BF16, (flags & KRPE_FEAT_ELU) != 0, a,
                                      static_cast<hipStream_t>(stream)),
                    "decay tree launch");
@@ -258,6 +257,7 @@ krpe_status_t krpe_decay_commit(const void* k, const void* v, int qkv_dtype, con
   clear_error();
   if (krpe_status_t s = check_pool(qkv_dtype, rate, W, state, slots, nslots, B, H, T, d, m, flags)) return s;
   if (P < 0) return fail(KRPE_ERR_SHAPE, "negative size");
+  if (T > 65536) return fail(KRPE_ERR_UNSUPPORTED, "more than 65536 tokens to choose from is not supported");
   const long long bh = static_cast<long long>(B) * H;
   if (bh * T == 0 || P == 0) return KRPE_OK;
   if (!k || !v || !path) return fail(KRPE_ERR_NULL, "k, v and path must be non-NULL");
@@ -268,8 +268,11 @@ krpe_status_t krpe_decay_commit(const void* k, const void* v, int qkv_dtype, con
                        {slots, slots ? B * sizeof(int) : 0}, {path, static_cast<size_t>(B) * P * sizeof(int)}};
   for (const Range& r : ins)
     if (overlaps({state, state_bytes(nslots, H, d, m)}, r)) return fail(KRPE_ERR_ALIAS, "the states overlap an input");
-  PoolArgs a = pool_args(nullptr, k, v, nullptr, rate, W, state, slots, nslots, B, H, d, m, flags);
-  a.tree = path, a.T = T, a.P = P;
+  DecayArgs a{};
+  a.k = k, a.v = v, a.rate = rate, a.W = W, a.state = state, a.slots = slots, a.path = path;
+  a.B = B, a.H = H, a.n = T, a.P = P, a.d = d, a.M = m, a.Mp = (m + 31) & ~31, a.nseg = 1;
+  a.nslots = nslots, a.nprf = (flags & KRPE_NPRF) != 0;
+  a.log2_m = -0.5 * std::log2(static_cast<double>(m));
   return hip_check(launch_decay_commit(qkv_dtype == KRPE_BF16, (flags & KRPE_FEAT_ELU) != 0, a,
                                        static_cast<hipStream_t>(stream)),
                    "decay commit launch");

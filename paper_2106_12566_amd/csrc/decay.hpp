@@ -55,96 +55,243 @@ __device__ __forceinline__ float decay(float rl, int dist) { return __builtin_am
 template <typename TX>
 constexpr int kTermsX = sizeof(TX) == 2 ? 1 : 3;
 
-// A lane's row (dimensions 16 ks + 8 lh + t) and its squared norm in fp64; zeros where !ok.
-template <typename TX, int DK>
-__device__ __forceinline__ double load_x(const TX* __restrict__ row, bool ok, int d, uint4 (&xf)[DK][kTermsX<TX>]) {
-  const int lh = (threadIdx.x & 63) >> 5;
-  const bool vec = d % 8 == 0;
-  double sq = 0.0;
-#pragma unroll
-  for (int ks = 0; ks < DK; ++ks) {
-    const int c = 16 * ks + 8 * lh;
-    float v8[8];
-    load8(row + (c < d ? c : 0), ok ? d - c : 0, vec, v8);
-#pragma unroll
-    for (int t = 0; t < 8; ++t) sq = fma(static_cast<double>(v8[t]), static_cast<double>(v8[t]), sq);
-    if constexpr (kTermsX<TX> == 1) {
-      xf[ks][0] = make_uint4(pack_bf16(floatx2{v8[0], v8[1]}), pack_bf16(floatx2{v8[2], v8[3]}), pack_bf16(floatx2{v8[4], v8[5]}),
-                             pack_bf16(floatx2{v8[6], v8[7]}));
+// Reads of rows of d elements through a buffer resource: offsets are in bytes from `base`, and what
+// lies at `bytes` or beyond (kOut among it) reads as zero.
+constexpr uint32_t kOut = 0x80000000u;
+template <typename T>
+struct Rows {
+  __amdgpu_buffer_rsrc_t r;
+  int d;
+  __device__ __forceinline__ Rows(const T* base, size_t count, int d_) : r(buffer_of(base, count * d_ * sizeof(T))), d(d_) {}
+  __device__ __forceinline__ uint32_t at(int row) const { return static_cast<uint32_t>(row) * static_cast<uint32_t>(d) * sizeof(T); }
+  // element c of the row at o (kOut past the row)
+  __device__ __forceinline__ uint32_t at(uint32_t o, int c) const { return c < d ? o + c * sizeof(T) : kOut; }
+  __device__ __forceinline__ float one(uint32_t o) const {
+    if constexpr (sizeof(T) == 2)
+      return to_f32(static_cast<uint16_t>(__builtin_amdgcn_raw_buffer_load_b16(r, o, 0, 0)));
+    else
+      return __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(r, o, 0, 0));
+  }
+  __device__ __forceinline__ uint4 b128(uint32_t o) const {
+    return __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(r, o, 0, 0));
+  }
+  __device__ __forceinline__ uint2 b64(uint32_t o) const {
+    return __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(r, o, 0, 0));
+  }
+};
+
+// Four elements from c of the row at o as they lie in memory (zeros past d).
+template <typename TX>
+struct Raw4 {
+  typename std::conditional<sizeof(TX) == 2, uint2, uint4>::type u;
+  __device__ __forceinline__ void load(const Rows<TX>& x, uint32_t o, int c) {
+    o = x.at(o, c);
+    if (x.d % 4 == 0) {
+      if constexpr (sizeof(TX) == 2)
+        u = x.b64(o);
+      else
+        u = x.b128(o);
     } else {
-      split_bf16x8(v8, xf[ks]);
+      float v[4];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        v[t] = x.one(o + t * sizeof(TX));
+        v[t] = c + t < x.d ? v[t] : 0.f;
+      }
+      if constexpr (sizeof(TX) == 2)
+        u = make_uint2(pack_bf16(floatx2{v[0], v[1]}), pack_bf16(floatx2{v[2], v[3]}));
+      else
+        u = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
     }
   }
-  return sq + __shfl_xor(sq, 32);
+  __device__ __forceinline__ void values(float (&v)[4]) const {
+    if constexpr (sizeof(TX) == 2) {
+      v[0] = __uint_as_float(u.x << 16), v[1] = __uint_as_float(u.x & 0xffff0000u);
+      v[2] = __uint_as_float(u.y << 16), v[3] = __uint_as_float(u.y & 0xffff0000u);
+    } else {
+      v[0] = __uint_as_float(u.x), v[1] = __uint_as_float(u.y), v[2] = __uint_as_float(u.z), v[3] = __uint_as_float(u.w);
+    }
+  }
+};
+template <typename TX>
+__device__ __forceinline__ void load4(const Rows<TX>& x, uint32_t o, int c, float (&v)[4]) {
+  Raw4<TX> r;
+  r.load(x, o, c);
+  r.values(v);
+}
+// Eight elements from c of the row at o as they lie in memory (zeros past d).
+template <typename TX>
+struct Raw8 {
+  uint4 u[sizeof(TX) / 2];
+  __device__ __forceinline__ void load(const Rows<TX>& x, uint32_t o, int c) {
+    o = x.at(o, c);
+    if (x.d % 8 == 0) {
+#pragma unroll
+      for (int i = 0; i < static_cast<int>(sizeof(TX) / 2); ++i) u[i] = x.b128(o + 16 * i);
+    } else {
+      float v[8];
+#pragma unroll
+      for (int t = 0; t < 8; ++t) {
+        v[t] = x.one(o + t * sizeof(TX));
+        v[t] = c + t < x.d ? v[t] : 0.f;
+      }
+      if constexpr (sizeof(TX) == 2) {
+        u[0] = make_uint4(pack_bf16(floatx2{v[0], v[1]}), pack_bf16(floatx2{v[2], v[3]}), pack_bf16(floatx2{v[4], v[5]}),
+                          pack_bf16(floatx2{v[6], v[7]}));
+      } else {
+        u[0] = make_uint4(__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3]));
+        u[1] = make_uint4(__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7]));
+      }
+    }
+  }
+  __device__ __forceinline__ void values(float (&v)[8]) const {
+    if constexpr (sizeof(TX) == 2) {
+      const unsigned w[4] = {u[0].x, u[0].y, u[0].z, u[0].w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) v[2 * j] = __uint_as_float(w[j] << 16), v[2 * j + 1] = __uint_as_float(w[j] & 0xffff0000u);
+    } else {
+      const unsigned w[8] = {u[0].x, u[0].y, u[0].z, u[0].w, u[1].x, u[1].y, u[1].z, u[1].w};
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(w[j]);
+    }
+  }
+  // the operand's terms (bf16: the elements themselves)
+  __device__ __forceinline__ void terms(uint4 (&t)[kTermsX<TX>]) const {
+    if constexpr (sizeof(TX) == 2) {
+      t[0] = u[0];
+    } else {
+      float v[8];
+      values(v);
+      split_bf16x8(v, t);
+    }
+  }
+};
+// A lane's row at o (dimensions 16 ks + 8 lh + t), fetched.
+template <typename TX, int DK>
+__device__ __forceinline__ void fetch_row(const Rows<TX>& rows, uint32_t o, Raw8<TX> (&x)[DK]) {
+  const int lh = (threadIdx.x & 63) >> 5;
+#pragma unroll
+  for (int ks = 0; ks < DK; ++ks) x[ks].load(rows, o, 16 * ks + 8 * lh);
+}
+// Its squared norm: in fp64 for fp32 rows, whose features are held whole; for bf16 ones in fp32,
+// in eight partial sums a lane (off by a few 2^-24 of itself).
+template <typename TX>
+using Sq = typename std::conditional<sizeof(TX) == 2, float, double>::type;
+template <typename TX, int DK>
+__device__ __forceinline__ Sq<TX> row_square(const Raw8<TX> (&x)[DK]) {
+  Sq<TX> p[8] = {};
+#pragma unroll
+  for (int ks = 0; ks < DK; ++ks) {
+    float v[8];
+    x[ks].values(v);
+#pragma unroll
+    for (int t = 0; t < 8; ++t) {
+      const Sq<TX> y = v[t];
+      p[t] = fma(y, y, p[t]);
+    }
+  }
+  const Sq<TX> s = ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+  return s + __shfl_xor(s, 32);
 }
 
 // What phi takes of a row: PRF phi_prf's r, c, f (features.hpp); elu + 1: the row's scale and 1.
 struct RowFactors {
   float r, c, f;
 };
-template <bool ELU>
-__device__ __forceinline__ RowFactors row_factors(double sq, bool nprf, double log2_m) {
-  const bool nz = sq > 0.0;
-  const double scale = nprf ? (nz ? 1.0 / sqrt(sq) : 0.0) : 1.0;
+template <bool ELU, typename S>
+__device__ __forceinline__ RowFactors row_factors(S sq, bool nprf, double log2_m) {
+  const bool nz = sq > 0;
+  S scale = 1;
+  if (nprf) scale = nz ? S(1) / sqrt(sq) : S(0);
   RowFactors o;
+  o.f = 1.f;
   if constexpr (ELU) {
-    o.r = static_cast<float>(scale), o.c = 0.f, o.f = 1.f;
+    o.r = static_cast<float>(scale), o.c = 0.f;
   } else {
-    const double c = log2_m - (nprf ? (nz ? 0.5 : 0.0) : 0.5 * sq) * kLog2e;
-    o.r = static_cast<float>(scale * kLog2e), o.c = static_cast<float>(c);
-    o.f = rounding_factor(c, o.c);
+    const S c = static_cast<S>(log2_m) - (nprf ? (nz ? S(0.5) : S(0)) : S(0.5) * sq) * static_cast<S>(kLog2e);
+    o.r = static_cast<float>(scale * static_cast<S>(kLog2e)), o.c = static_cast<float>(c);
+    if constexpr (sizeof(S) == 8) o.f = rounding_factor(c, o.c);
   }
   return o;
 }
-template <bool ELU>
+// WHOLE: the projection in two accumulators and the exponent's rounding made good (fp32 rows).
+template <bool ELU, bool WHOLE>
 __device__ __forceinline__ float feature(float s, float sl, float r, float c, float f) {
+  if constexpr (WHOLE) s += sl;
   if constexpr (ELU) {
-    const float x = (s + sl) * r;
+    const float x = s * r;
     return (x > 0.f ? x + 1.f : __builtin_amdgcn_exp2f(x * 1.44269504f)) * f;
   } else {
-    return phi_prf(s, sl, r, c, f);
+    const float y = __builtin_amdgcn_exp2f(fmaf(s, r, c));
+    return WHOLE ? y * f : y;
   }
 }
 
-// 32 rows of W from f0 as operands wf[ks][term][64] in LDS (zeros past m; elu + 1: rows of the identity).
+// 32 rows of W from f0 as operands wf[ks][term][64] in LDS (zeros past m; elu + 1: rows of the
+// identity), fetched by a work-group of 256 threads and put a step later.
+// (W's rows past m read as zeros)
+template <bool ELU>
+__device__ __forceinline__ void load_weights(const Rows<float>& W, int f, int c, float (&v)[8]) {
+  if constexpr (ELU) {
+#pragma unroll
+    for (int t = 0; t < 8; ++t) v[t] = c + t == f ? 1.f : 0.f;
+  } else {
+    float u[4];
+    load4(W, W.at(f), c, u);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) v[t] = u[t];
+    load4(W, W.at(f), c + 4, u);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) v[4 + t] = u[t];
+  }
+}
 template <int DK, int NW, bool ELU>
-__device__ __forceinline__ void stage_weights(const float* __restrict__ W, int f0, int m, int d, uint4* __restrict__ wf) {
-  for (int e = threadIdx.x; e < 32 * 2 * DK; e += blockDim.x) {
-    const int fl = e / (2 * DK), c = e % (2 * DK), f = f0 + fl;
-    float v8[8];
-    if constexpr (ELU) {
+struct WeightTile {
+  static constexpr int N = 32 * 2 * DK / 256 > 0 ? 32 * 2 * DK / 256 : 1;
+  float v[N][8];
+  __device__ __forceinline__ void fetch(const Rows<float>& W, int f0) {
 #pragma unroll
-      for (int t = 0; t < 8; ++t) v8[t] = 8 * c + t == f ? 1.f : 0.f;
-    } else {
-      load8(W + static_cast<size_t>(min(f, m - 1)) * d + min(8 * c, d - 1), f < m ? d - 8 * c : 0, d % 4 == 0, v8);
+    for (int i = 0; i < N; ++i) {
+      const int e = threadIdx.x + 256 * i;
+      if (DK * 64 < 256 && e >= 64 * DK) return;
+      load_weights<ELU>(W, f0 + e / (2 * DK), 8 * (e % (2 * DK)), v[i]);
     }
-    uint4 t3[3];
-    split_bf16x8(v8, t3);
-    uint4* __restrict__ o = wf + (c >> 1) * NW * kFragLanes + (c & 1) * 32 + fl;
-#pragma unroll
-    for (int s = 0; s < NW; ++s) o[s * kFragLanes] = t3[s];
   }
-}
+  __device__ __forceinline__ void put(uint4* __restrict__ wf) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int e = threadIdx.x + 256 * i, fl = e / (2 * DK), c = e % (2 * DK);
+      if (DK * 64 < 256 && fl >= 32) return;
+      uint4 t3[3];
+      split_bf16x8(v[i], t3);
+      uint4* __restrict__ o = wf + (c >> 1) * NW * kFragLanes + (c & 1) * 32 + fl;
+#pragma unroll
+      for (int s = 0; s < NW; ++s) o[s * kFragLanes] = t3[s];
+    }
+  }
+};
 
-// Projections of 32 rows on 32 features (project of features.hpp with NW terms of W): the
-// products of the largest terms and the others apart.
-template <int DK, int NSX, int NW, bool XROWS>
-__device__ __forceinline__ void project_terms(const uint4* __restrict__ wf, const uint4 (&xf)[DK][NSX], floatx16& acc,
-                                              floatx16& lo) {
-  const int lane = threadIdx.x & 63;
+// Projections of 32 rows on 32 features: with WHOLE the products of the largest terms (acc) and
+// the others (lo) apart, else in one sum, the small ones first.
+template <int DK, int NSX, int NW, bool XROWS, bool WHOLE, typename F>
+__device__ __forceinline__ void project_terms(F&& weights, const uint4 (&xf)[DK][NSX], floatx16& acc, floatx16& lo) {
   acc = zero16();
-  lo = zero16();
+  if constexpr (WHOLE) lo = zero16();
   auto mul = [](uint4 w, uint4 x, floatx16 c) { return XROWS ? mfma_bf16(x, w, c) : mfma_bf16(w, x, c); };
 #pragma unroll
   for (int ks = 0; ks < DK; ++ks) {
     uint4 w[NW];
-#pragma unroll
-    for (int s = 0; s < NW; ++s) w[s] = wf[(ks * NW + s) * kFragLanes + lane];
+    weights(ks, w);
 #pragma unroll
     for (int s = 2; s >= 1; --s)
 #pragma unroll
       for (int i = 0; i <= s; ++i)
-        if (i < NW && s - i < NSX) lo = mul(w[i], xf[ks][s - i], lo);
+        if (i < NW && s - i < NSX) {
+          if constexpr (WHOLE)
+            lo = mul(w[i], xf[ks][s - i], lo);
+          else
+            acc = mul(w[i], xf[ks][s - i], acc);
+        }
     acc = mul(w[0], xf[ks][0], acc);
   }
 }
@@ -188,23 +335,6 @@ __device__ __forceinline__ void read_terms(const uint4* __restrict__ p, uint4 (&
   for (int s = 0; s < N; ++s) t[s] = p[s * kFragLanes + (threadIdx.x & 63)];
 }
 
-// Four values of a row from column c (zeros past d, or all of them where !ok).
-template <typename TX>
-__device__ __forceinline__ void load4(const TX* __restrict__ row, int c, bool ok, int d, float (&v)[4]) {
-  if (ok && d % 4 == 0 && c < d) {
-    if constexpr (std::is_same<TX, float>::value) {
-      const float4 u = *reinterpret_cast<const float4*>(row + c);
-      v[0] = u.x, v[1] = u.y, v[2] = u.z, v[3] = u.w;
-    } else {
-      const uint2 u = *reinterpret_cast<const uint2*>(row + c);
-      v[0] = __uint_as_float(u.x << 16), v[1] = __uint_as_float(u.x & 0xffff0000u);
-      v[2] = __uint_as_float(u.y << 16), v[3] = __uint_as_float(u.y & 0xffff0000u);
-    }
-  } else {
-#pragma unroll
-    for (int t = 0; t < 4; ++t) v[t] = ok && c + t < d ? to_f32(row[c + t]) : 0.f;
-  }
-}
 template <typename TZ>
 __device__ __forceinline__ void store4(TZ* __restrict__ row, int c, int d, const float (&v)[4]) {
   if (d % 4 == 0 && c < d) {
@@ -226,47 +356,70 @@ __device__ __forceinline__ void store4(TZ* __restrict__ row, int c, int d, const
 
 __device__ __forceinline__ bool finite(float v) { return fabsf(v) <= 3.4028235e38f; }
 
-// Rows p0 .. p0 + 32 blocks - 1 of a [.][d] array turned into Z fragments (column 32 ct + lr,
-// positions along the slots) vf[block][ct][k2][term][64], zeros past `rows` rows and past d.
-// CLEAN: a value that is not finite goes in as zero and sets *odd, as a product with a weight of
-// zero would carry it to rows that do not see it; MARK: 1 for such values and 0 for others.
+// Rows of a [.][d] array turned into Z fragments (column 32 ct + lr, positions along the slots)
+// vf[block][ct][k2][term][64], zeros past the array's end and past d: patches of four rows and four
+// columns, fetched by a work-group of THREADS and put a step later.
+// kClean: a value that is not finite goes in as zero and sets *odd, as a product with a weight of
+// zero would carry it to rows that do not see it; kMark: 1 for such values and 0 for others.
 enum class Values { kAsIs, kClean, kMark };
-template <typename TX, int DT, int NT, Values MODE>
-__device__ __forceinline__ void stage_columns(const TX* __restrict__ v, int p0, int rows, int d, int blocks,
-                                              uint4* __restrict__ vf, int* __restrict__ odd) {
-  for (int e = threadIdx.x; e < blocks * 8 * DT * 8; e += blockDim.x) {
-    const int cg = e % (DT * 8), g = (e / (DT * 8)) % 8, blk = e / (DT * 64);
-    const int c = 4 * cg, r0 = 32 * blk + 4 * g;
-    float val[4][4];
+template <typename TX, int DT, int BLOCKS, int THREADS>
+struct ColumnTile {
+  static constexpr int N = (BLOCKS * 64 * DT + THREADS - 1) / THREADS;
+  Raw4<TX> v[N][4];
+  // row(r): where row r of the tile lies (kOut: zeros)
+  template <typename F>
+  __device__ __forceinline__ void fetch(const Rows<TX>& x, F&& row) {
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
-      load4(v + static_cast<size_t>(p0 + min(r0 + r, rows - 1)) * d, c, r0 + r < rows, d, val[r]);
-    if constexpr (MODE != Values::kAsIs) {
-      bool bad = false;
+    for (int i = 0; i < N; ++i) {
+      const int e = threadIdx.x + THREADS * i, cg = e % (DT * 8), r0 = 4 * (e / (DT * 8));
 #pragma unroll
-      for (int r = 0; r < 4; ++r)
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          const bool f = finite(val[r][t]);
-          bad |= !f;
-          if constexpr (MODE == Values::kMark)
-            val[r][t] = f ? 0.f : 1.f;
-          else
-            val[r][t] = f ? val[r][t] : 0.f;
-        }
-      if (MODE == Values::kClean && bad) *odd = 1;
-    }
-    uint2* __restrict__ o = reinterpret_cast<uint2*>(
-        vf + (((blk * DT + (c >> 5)) * 2 + (g >> 2)) * NT) * kFragLanes + (g & 1) * 32 + (c & 31));
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      uint32_t a[NT], b[NT];
-      split_pair<NT>(val[0][t], val[1][t], a);
-      split_pair<NT>(val[2][t], val[3][t], b);
-#pragma unroll
-      for (int s = 0; s < NT; ++s) o[2 * (s * kFragLanes + t) + ((g >> 1) & 1)] = make_uint2(a[s], b[s]);
+      for (int r = 0; r < 4; ++r) v[i][r].load(x, row(r0 + r), 4 * cg);
     }
   }
+  template <int NT, Values MODE>
+  __device__ __forceinline__ void put(uint4* __restrict__ vf, int* __restrict__ odd) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int e = threadIdx.x + THREADS * i;
+      const int cg = e % (DT * 8), g = (e / (DT * 8)) % 8, blk = e / (DT * 64);
+      const int c = 4 * cg;
+      if (N * THREADS > BLOCKS * 64 * DT && blk >= BLOCKS) return;
+      float val[4][4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) v[i][r].values(val[r]);
+      if constexpr (MODE != Values::kAsIs) {
+        bool bad = false;
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+          for (int t = 0; t < 4; ++t) {
+            const bool f = finite(val[r][t]);
+            bad |= !f;
+            if constexpr (MODE == Values::kMark)
+              val[r][t] = f ? 0.f : 1.f;
+            else
+              val[r][t] = f ? val[r][t] : 0.f;
+          }
+        if (MODE == Values::kClean && bad) *odd = 1;
+      }
+      uint2* __restrict__ o = reinterpret_cast<uint2*>(
+          vf + (((blk * DT + (c >> 5)) * 2 + (g >> 2)) * NT) * kFragLanes + (g & 1) * 32 + (c & 31));
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        uint32_t a[NT], b[NT];
+        split_pair<NT>(val[0][t], val[1][t], a);
+        split_pair<NT>(val[2][t], val[3][t], b);
+#pragma unroll
+        for (int s = 0; s < NT; ++s) o[2 * (s * kFragLanes + t) + ((g >> 1) & 1)] = make_uint2(a[s], b[s]);
+      }
+    }
+  }
+};
+template <typename TX, int DT, int BLOCKS, int NT, Values MODE>
+__device__ __forceinline__ void stage_columns(const Rows<TX>& x, uint4* __restrict__ vf, int* __restrict__ odd) {
+  ColumnTile<TX, DT, BLOCKS, 256> t;
+  t.fetch(x, [&](int r) { return x.at(r); });
+  t.template put<NT, MODE>(vf, odd);
 }
 
 // ---- the prompts' passes
@@ -276,37 +429,103 @@ struct DecayArgs {
   const float *rate, *W;
   float* state;         // pool [nslots][H][d + 1][M], or NULL
   const int *slots, *lens;
-  float* tot;           // [BH][nseg][d + 1][Mp]: a segment's sums at its end, then the state before it
-  float* pre;           // [BH][nchunk][d + 1][Mp]: sums of the segment before each of its chunks
-  // gradients: dz; dq, dk, dv; [dL/dnumerators | dL/ddenominator] of the rows, g [BH][n][d] and
+  // One segment (nseg == 1): pre [BH][nchunk][d + 1][Mp] is the state before each chunk.  More:
+  // pre is the sums of the segment before each of its chunks but the first, tot [BH][nseg][d + 1][Mp]
+  // a segment's sums at its end, and after the join the state before it.
+  float *tot, *pre;
+  const int* path;      // [B][P]: the rows of k, v to take (krpe_decay_commit)
+  // gradients: dz; dq, dk, dv; [dL/dnumerator | dL/ddenominator] of the rows, g [BH][n][d] and
   // gd [BH][n]; the queries' sums backwards in time, totb and preb as tot and pre
   const void* dz;
   void *dq, *dk, *dv;
   float *g, *gd, *totb, *preb;
-  int B, H, n, d, M, Mp, nchunk, nseg, segc, nslots, nprf, fresh;
+  int B, H, n, d, M, Mp, nchunk, nseg, segc, nslots, nprf, fresh, P;
   double log2_m;
-};
-// ---- calls on a pool of states
-struct PoolArgs {
-  const void *q, *k, *v;
-  void* z;
-  const float *rate, *W;
-  float* state;             // [nslots][H][d + 1][M]
-  const int *slots, *tree;  // tree: parents [B][T] (tree), accepted nodes [B][P] (commit)
-  int B, H, T, P, d, M, nslots, nprf;
-  float log_m;              // -log(sqrt(m))
-  double log2_m;            // -log2(sqrt(m))
 };
 __device__ __forceinline__ int rows_of(const int* __restrict__ lens, int b, int n) {
   return lens ? min(max(lens[b], 0), n) : n;
 }
 
+// The state outside a chunk, wold old + pre (either may be NULL), fetched 32 features at a time.
+// As rows: operands sl[ct][ks][term][64], lane: column, features in the slots' order.  As columns:
+// sl[ks][term][64], lane: feature, columns in the slots' order.
+template <int DT, int NT, bool COLUMNS>
+struct StateTile {
+  static constexpr int ITEMS = DT * 128, N = (ITEMS + 255) / 256;
+  const float *old, *pre;
+  float wold;
+  int d, Mp;
+  float o[N][8], p[N][8], so, sp;
+  __device__ __forceinline__ StateTile(const float* old_, const float* pre_, float w, int d_, int Mp_)
+      : old(old_), pre(pre_), wold(w), d(d_), Mp(Mp_), so(0.f), sp(0.f) {}
+  __device__ __forceinline__ bool any() const { return old || pre; }
+  __device__ __forceinline__ void read(const float* __restrict__ from, int f0, float (&x)[N][8], float& last) const {
+    const Rows<float> r(from, d + 1, Mp);
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int e = threadIdx.x + 256 * n;
+      if (N * 256 > ITEMS && e >= ITEMS) break;
+      if constexpr (COLUMNS) {
+        const int l = e & 31, half = (e >> 5) & 1, ks = e >> 6;
+#pragma unroll
+        for (int t = 0; t < 8; ++t) {
+          const int c = 16 * ks + 8 * (t >> 2) + 4 * half + (t & 3);
+          x[n][t] = r.one(c < d ? r.at(c) + 4u * (f0 + l) : kOut);
+        }
+      } else {
+        const int c = e >> 2, ks = (e >> 1) & 1, half = e & 1;
+        const uint32_t at = c < d ? r.at(c) + 4u * (f0 + 16 * ks + 4 * half) : kOut;
+        const uint4 u = r.b128(at), w = r.b128(at + 32);
+        x[n][0] = __uint_as_float(u.x), x[n][1] = __uint_as_float(u.y), x[n][2] = __uint_as_float(u.z), x[n][3] = __uint_as_float(u.w);
+        x[n][4] = __uint_as_float(w.x), x[n][5] = __uint_as_float(w.y), x[n][6] = __uint_as_float(w.z), x[n][7] = __uint_as_float(w.w);
+      }
+    }
+    if (threadIdx.x < 32) last = from[static_cast<size_t>(d) * Mp + f0 + threadIdx.x];
+  }
+  __device__ __forceinline__ void fetch(int f0) {
+    if (old) read(old, f0, o, so);
+    if (pre) read(pre, f0, p, sp);
+  }
+  __device__ __forceinline__ void put(uint4* __restrict__ sl, float* __restrict__ sden) const {
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int e = threadIdx.x + 256 * n;
+      if (N * 256 > ITEMS && e >= ITEMS) break;
+      float x[8];
+#pragma unroll
+      for (int t = 0; t < 8; ++t) x[t] = old ? (pre ? fmaf(wold, o[n][t], p[n][t]) : wold * o[n][t]) : p[n][t];
+      uint32_t q[4][NT];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) split_pair<NT>(x[2 * j], x[2 * j + 1], q[j]);
+      int at;
+      if constexpr (COLUMNS)
+        at = (e >> 6) * NT * kFragLanes + (e & 63);
+      else
+        at = (((e >> 7) * 2 + ((e >> 1) & 1)) * NT) * kFragLanes + 32 * (e & 1) + ((e >> 2) & 31);
+#pragma unroll
+      for (int s = 0; s < NT; ++s) sl[at + s * kFragLanes] = make_uint4(q[0][s], q[1][s], q[2][s], q[3][s]);
+    }
+    if (threadIdx.x < 32) sden[threadIdx.x] = (old ? wold * so : 0.f) + (pre ? sp : 0.f);
+  }
+};
+
+// ---- calls on a pool of states
+struct PoolArgs {
+  const void *q, *k, *v;
+  void* z;
+  const float *rate, *W;
+  float* state;               // [nslots][H][d + 1][M]
+  const int *slots, *parent;  // parent [B][T]
+  int B, H, T, d, M, nslots, nprf;
+  float log_m;                // -log(sqrt(m))
+  double log2_m;              // -log2(sqrt(m))
+};
 // Host-side launchers (decay_fwd.hip, decay_bwd.hip, decay_step.hip, decay_tree.hip).
 hipError_t launch_decay_fwd(bool bf16, bool elu, const DecayArgs& a, hipStream_t st);
 hipError_t launch_decay_bwd(bool bf16, bool elu, const DecayArgs& a, hipStream_t st);
 hipError_t launch_decay_step(bool bf16, bool elu, const PoolArgs& a, hipStream_t st);
 hipError_t launch_decay_tree(bool bf16, bool elu, const PoolArgs& a, hipStream_t st);
-hipError_t launch_decay_commit(bool bf16, bool elu, const PoolArgs& a, hipStream_t st);
+hipError_t launch_decay_commit(bool bf16, bool elu, const DecayArgs& a, hipStream_t st);
 hipError_t launch_state_copy(float* state, const int* src, const int* dst, int count, int nslots, long long cells,
                              hipStream_t st);
 

@@ -20,16 +20,16 @@
 
 namespace krpe {
 
-// Rows p0 .. p0 + 127 as operands over their columns: f[tile][ks][term][64], lane: row, column
-// 16 ks + 8 (t / 4) + 4 lh + t % 4; zeros past `rows` rows and past d.
+// 128 rows as operands over their columns: f[tile][ks][term][64], lane: row, column
+// 16 ks + 8 (t / 4) + 4 lh + t % 4; zeros past the array's end and past d.
 template <typename T, int DK, int NT>
-__device__ __forceinline__ void stage_rows(const T* __restrict__ x, int p0, int rows, int d, uint4* __restrict__ f) {
-  for (int e = threadIdx.x; e < 128 * DK * 2; e += 256) {
-    const int half = e & 1, ks = (e >> 1) % DK, r = e / (2 * DK);
-    const T* __restrict__ row = x + static_cast<size_t>(p0 + min(r, rows - 1)) * d;
+__device__ __forceinline__ void stage_rows(const Rows<T>& x, uint4* __restrict__ f) {
+#pragma unroll
+  for (int n = 0; n < DK; ++n) {
+    const int e = threadIdx.x + 256 * n, half = e & 1, ks = (e >> 1) % DK, r = e / (2 * DK);
     float u[4], w[4];
-    load4(row, 16 * ks + 4 * half, r < rows, d, u);
-    load4(row, 16 * ks + 4 * half + 8, r < rows, d, w);
+    load4(x, x.at(r), 16 * ks + 4 * half, u);
+    load4(x, x.at(r), 16 * ks + 4 * half + 8, w);
     uint32_t p[4][NT];
     split_pair<NT>(u[0], u[1], p[0]), split_pair<NT>(u[2], u[3], p[1]);
     split_pair<NT>(w[0], w[1], p[2]), split_pair<NT>(w[2], w[3], p[3]);
@@ -39,11 +39,48 @@ __device__ __forceinline__ void stage_rows(const T* __restrict__ x, int p0, int 
   }
 }
 
+// 32 rows of W from f0 turned: operands tl[ct][k2][term][64], lane: dimension, features in the
+// slots (elu + 1: the identity).
+template <int DT, int NT, bool ELU>
+struct TurnedTile {
+  static constexpr int N = (DT * 128 + 255) / 256;
+  float v[N][8];
+  __device__ __forceinline__ void fetch(const Rows<float>& W, int f0) {
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int e = threadIdx.x + 256 * n, c = e % (32 * DT), half = (e / (32 * DT)) & 1, k2 = e / (64 * DT);
+      if (N * 256 > DT * 128 && e >= DT * 128) break;
+#pragma unroll
+      for (int t = 0; t < 8; ++t) {
+        const int l = f0 + 16 * k2 + 8 * (t >> 2) + 4 * half + (t & 3);
+        if constexpr (ELU)
+          v[n][t] = l == c ? 1.f : 0.f;
+        else
+          v[n][t] = W.one(W.at(W.at(l), c));
+      }
+    }
+  }
+  __device__ __forceinline__ void put(uint4* __restrict__ tl) const {
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+      const int e = threadIdx.x + 256 * n, c = e % (32 * DT), half = (e / (32 * DT)) & 1, k2 = e / (64 * DT);
+      if (N * 256 > DT * 128 && e >= DT * 128) break;
+      uint32_t q[4][NT];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) split_pair<NT>(v[n][2 * j], v[n][2 * j + 1], q[j]);
+#pragma unroll
+      for (int s = 0; s < NT; ++s)
+        tl[(((c >> 5) * 2 + k2) * NT + s) * kFragLanes + 32 * half + (c & 31)] = make_uint4(q[0][s], q[1][s], q[2][s], q[3][s]);
+    }
+  }
+};
+
 // Gradient of a lane's row (columns 32 t + 8 g + 4 lh + j along the registers) from
 // y = W^T p (elu + 1: p itself) and sum(p).
 template <typename TX, int DT, bool ELU>
-__device__ __forceinline__ void store_row_gradient(const TX* __restrict__ x, floatx16 (&y)[DT], float sum, TX* __restrict__ o,
-                                                   bool ok, int d, bool nprf) {
+__device__ __forceinline__ void store_row_gradient(const Rows<TX>& x, uint32_t at, floatx16 (&y)[DT], float sum,
+                                                   TX* __restrict__ o, bool ok, bool nprf) {
+  const int d = x.d;
   const int lh = (threadIdx.x & 63) >> 5;
   float xv[DT][16];
   float sq = 0.f;
@@ -52,7 +89,7 @@ __device__ __forceinline__ void store_row_gradient(const TX* __restrict__ x, flo
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
       float u[4];
-      load4(x, 32 * t + 8 * g + 4 * lh, true, d, u);
+      load4(x, at, 32 * t + 8 * g + 4 * lh, u);
 #pragma unroll
       for (int j = 0; j < 4; ++j) xv[t][4 * g + j] = u[j], sq = fmaf(u[j], u[j], sq);
     }
@@ -86,6 +123,7 @@ __device__ __forceinline__ void store_row_gradient(const TX* __restrict__ x, flo
 template <typename TX, int DK, int NT, int SIDE, bool ELU>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k_decay_grad(DecayArgs a) {
   using TG = typename std::conditional<SIDE == 0, TX, float>::type;  // values of the other rows: v, or g
+  constexpr bool WHOLE = sizeof(TX) == 4;
   constexpr int NSX = kTermsX<TX>, DT = DK / 2, NW = 3;
   extern __shared__ __align__(16) uint4 smem[];
   // first pass                                        second pass
@@ -102,27 +140,38 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k
   if (cnt <= 0) return;
   const size_t base = static_cast<size_t>(bh) * a.n * d, cells = static_cast<size_t>(d + 1) * a.Mp;
   const float rl = rate_log2(a.rate[h]);
-  const float* __restrict__ W = a.W + static_cast<size_t>(h) * a.M * d;
+  const Rows<float> W(a.W + static_cast<size_t>(h) * a.M * d, a.M, d);
   const int seg = ch / a.segc, c0 = seg * a.segc, c1 = min(min(a.nchunk, c0 + a.segc), (rows + kChunk - 1) / kChunk);
   const bool inner = SIDE == 0 ? ch > c0 : ch + 1 < c1;
   const float* __restrict__ pre = inner ? (SIDE == 0 ? a.pre : a.preb) + (static_cast<size_t>(bh) * a.nchunk + ch) * cells : nullptr;
-  const float* __restrict__ old = (SIDE == 0 ? a.tot : a.totb) + (static_cast<size_t>(bh) * a.nseg + seg) * cells;
+  const float* __restrict__ old =
+      a.nseg > 1 ? (SIDE == 0 ? a.tot : a.totb) + (static_cast<size_t>(bh) * a.nseg + seg) * cells : nullptr;
   const float wold = decay(rl, SIDE == 0 ? (ch - c0) * kChunk : min(rows, c1 * kChunk) - (p0 + cnt));
   const int i = 32 * wave + lr;  // the lane's own row
   const float share = decay(rl, SIDE == 0 ? i + 1 : cnt - min(i, cnt));  // of the state outside the chunk
-  const size_t row = static_cast<size_t>(p0 + min(i, cnt - 1)) * d;
-  const TX* __restrict__ own = static_cast<const TX*>(SIDE == 0 ? a.q : a.k) + base + row;
-  const TX* __restrict__ oth = static_cast<const TX*>(SIDE == 0 ? a.k : a.q) + base + row;
-  const TG* __restrict__ vals = (SIDE == 0 ? static_cast<const TG*>(a.v) : reinterpret_cast<const TG*>(a.g)) + base;
+  const size_t from = base + static_cast<size_t>(p0) * d;
+  const Rows<TX> own(static_cast<const TX*>(SIDE == 0 ? a.q : a.k) + from, cnt, d);
+  const Rows<TX> oth(static_cast<const TX*>(SIDE == 0 ? a.k : a.q) + from, cnt, d);
+  const Rows<TG> vals((SIDE == 0 ? static_cast<const TG*>(a.v) : reinterpret_cast<const TG*>(a.g)) + from, cnt, d);
   auto uses = [&](int t) { return SIDE == 0 ? t <= wave : t >= wave; };  // tiles of the other rows
   auto weight = [&](int t, int e) {
     const int j = 32 * t + 8 * (e >> 2) + 4 * lh + (e & 3);
     const int dist = SIDE == 0 ? i - j : j - i;
     return dist >= 0 ? decay(rl, dist) : 0.f;
   };
+  WeightTile<DK, NW, ELU> wt;
   uint4 of[DK][NSX], tf[DK][NSX];
-  const RowFactors fo = row_factors<ELU>(load_x<TX, DK>(own, i < cnt, d, of), a.nprf, a.log2_m);
-  const RowFactors ft = row_factors<ELU>(load_x<TX, DK>(oth, i < cnt, d, tf), a.nprf, a.log2_m);
+  RowFactors fo, ft;
+  {
+    Raw8<TX> x[DK], y[DK];
+    fetch_row<TX, DK>(own, own.at(i), x);
+    fetch_row<TX, DK>(oth, oth.at(i), y);
+    fo = row_factors<ELU>(row_square<TX, DK>(x), a.nprf, a.log2_m);
+    ft = row_factors<ELU>(row_square<TX, DK>(y), a.nprf, a.log2_m);
+#pragma unroll
+    for (int ks = 0; ks < DK; ++ks) x[ks].terms(of[ks]), y[ks].terms(tf[ks]);
+  }
+  auto weights = [&](int ks, uint4(&w)[NW]) { read_terms<NW>(wl + ks * NW * kFragLanes, w); };
   // [g | gd] of the lane's row (SIDE 0), or its values (SIDE 1)
   floatx16 G[DT];
   float gd = 1.f;
@@ -133,36 +182,25 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k
 #pragma unroll
     for (int t = 0; t < DT; ++t) Z[t] = zero16();
     float den = 0.f;
+    StateTile<DT, NT, false> state(old, pre, wold, d, a.Mp);
+    wt.fetch(W, 0);
+    state.fetch(0);
+#pragma unroll 1
     for (int f0 = 0; f0 < a.Mp; f0 += 32) {
-      __syncthreads();
-      stage_weights<DK, NW, ELU>(W, f0, a.M, d, wl);
-      for (int e = threadIdx.x; e < DT * 32 * 4; e += 256) {
-        const int c = e >> 2, ks = (e >> 1) & 1, half = e & 1;
-        floatx16 x = zero16();  // (eight used)
-        if (c < d) {
-          const size_t at = static_cast<size_t>(c) * a.Mp + f0 + 16 * ks + 4 * half;
-#pragma unroll
-          for (int t = 0; t < 8; ++t) {
-            const size_t p = at + (t & 3) + 8 * (t >> 2);
-            x[t] = wold * old[p] + (pre ? pre[p] : 0.f);
-          }
-        }
-        uint4 t[NT];
-        pack_half<NT>(x, 0, t);
-#pragma unroll
-        for (int s = 0; s < NT; ++s) sl[(((c >> 5) * 2 + ks) * NT + s) * kFragLanes + 32 * half + (c & 31)] = t[s];
-      }
-      if (threadIdx.x < 32) {
-        const size_t at = static_cast<size_t>(d) * a.Mp + f0 + threadIdx.x;
-        sden[threadIdx.x] = wold * old[at] + (pre ? pre[at] : 0.f);
+      // (the waves have all read the operands before: they have passed the barrier after phi)
+      wt.put(wl);
+      if (state.any()) state.put(sl, sden);
+      if (f0 + 32 < a.Mp) {
+        wt.fetch(W, f0 + 32);
+        state.fetch(f0 + 32);
       }
       __syncthreads();
       floatx16 acc, lo, ph;
       const bool part = f0 + 32 > a.M;
-      project_terms<DK, NSX, NW, false>(wl, tf, acc, lo);
+      project_terms<DK, NSX, NW, false, WHOLE>(weights, tf, acc, lo);
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        ph[e] = feature<ELU>(acc[e], lo[e], ft.r, ft.c, ft.f);
+        ph[e] = feature<ELU, WHOLE>(acc[e], WHOLE ? lo[e] : 0.f, ft.r, ft.c, ft.f);
         if (part && f0 + 8 * (e >> 2) + 4 * lh + (e & 3) >= a.M) ph[e] = 0.f;
       }
 #pragma unroll
@@ -172,27 +210,29 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k
 #pragma unroll
         for (int s = 0; s < NT; ++s) kl[((wave * 2 + k2) * NT + s) * kFragLanes + lane] = t[s];
       }
-      project_terms<DK, NSX, NW, false>(wl, of, acc, lo);
+      project_terms<DK, NSX, NW, false, WHOLE>(weights, of, acc, lo);
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        ph[e] = feature<ELU>(acc[e], lo[e], fo.r, fo.c, fo.f);
+        ph[e] = feature<ELU, WHOLE>(acc[e], WHOLE ? lo[e] : 0.f, fo.r, fo.c, fo.f);
         if (part && f0 + 8 * (e >> 2) + 4 * lh + (e & 3) >= a.M) ph[e] = 0.f;
       }
       uint4 po[2][NT];
       pack_half<NT>(ph, 0, po[0]);
       pack_half<NT>(ph, 1, po[1]);
-      if constexpr (SIDE == 0) {
+      if (state.any()) {
+        if constexpr (SIDE == 0) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) den = fmaf(sden[8 * (e >> 2) + 4 * lh + (e & 3)], ph[e], den);
-      }
-#pragma unroll
-      for (int ct = 0; ct < DT; ++ct)
-#pragma unroll
-        for (int k2 = 0; k2 < 2; ++k2) {
-          uint4 t[NT];
-          read_terms<NT>(sl + (ct * 2 + k2) * NT * kFragLanes, t);
-          Z[ct] = mfma_terms<NT, NT>(t, po[k2], Z[ct]);
+          for (int e = 0; e < 16; ++e) den = fmaf(sden[8 * (e >> 2) + 4 * lh + (e & 3)], ph[e], den);
         }
+#pragma unroll
+        for (int ct = 0; ct < DT; ++ct)
+#pragma unroll
+          for (int k2 = 0; k2 < 2; ++k2) {
+            uint4 t[NT];
+            read_terms<NT>(sl + (ct * 2 + k2) * NT * kFragLanes, t);
+            Z[ct] = mfma_terms<NT, NT>(t, po[k2], Z[ct]);
+          }
+      }
       __syncthreads();
 #pragma unroll
       for (int t = 0; t < 4; ++t)
@@ -211,7 +251,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k
 #pragma unroll
       for (int e = 0; e < 16; ++e) Z[ct][e] *= share;
     __syncthreads();
-    stage_columns<TG, DT, NT, Values::kAsIs>(vals, p0, cnt, d, 4, vl, nullptr);
+    stage_columns<TG, DT, 4, NT, Values::kAsIs>(vals, vl, nullptr);
     if (SIDE == 1 && threadIdx.x < kChunk)
       sgd[threadIdx.x] = static_cast<int>(threadIdx.x) < cnt ? a.gd[static_cast<size_t>(bh) * a.n + p0 + threadIdx.x] : 0.f;
     __syncthreads();
@@ -238,8 +278,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k
     if constexpr (SIDE == 0) {
       den += __shfl_xor(den, 32);
       const float inv = i < cnt ? 1.f / den : 0.f;
-      const TX* __restrict__ dz = static_cast<const TX*>(a.dz) + base + row;
-      float* __restrict__ g = a.g + base + row;
+      const Rows<TX> dz(static_cast<const TX*>(a.dz) + from, cnt, d);
+      float* __restrict__ g = a.g + from + static_cast<size_t>(i) * d;
       float dot = 0.f;
 #pragma unroll
       for (int ct = 0; ct < DT; ++ct)
@@ -247,7 +287,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k
         for (int g4 = 0; g4 < 4; ++g4) {
           const int c = 32 * ct + 8 * g4 + 4 * lh;
           float u[4];
-          load4(dz, c, i < cnt, d, u);
+          load4(dz, dz.at(i), c, u);
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             u[j] *= inv;
@@ -259,15 +299,15 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k
       gd = -(dot + __shfl_xor(dot, 32)) * inv;
       if (i < cnt && lh == 0) a.gd[static_cast<size_t>(bh) * a.n + p0 + i] = gd;
     } else {
-      const TX* __restrict__ v = static_cast<const TX*>(a.v) + base + row;
-      TX* __restrict__ dv = static_cast<TX*>(a.dv) + base + row;
+      const Rows<TX> v(static_cast<const TX*>(a.v) + from, cnt, d);
+      TX* __restrict__ dv = static_cast<TX*>(a.dv) + from + static_cast<size_t>(i) * d;
 #pragma unroll
       for (int ct = 0; ct < DT; ++ct)
 #pragma unroll
         for (int g4 = 0; g4 < 4; ++g4) {
           const int c = 32 * ct + 8 * g4 + 4 * lh;
           float u[4];
-          load4(v, c, i < cnt, d, u);
+          load4(v, v.at(i), c, u);
 #pragma unroll
           for (int j = 0; j < 4; ++j) G[ct][4 * g4 + j] = u[j];
           const float o[4] = {Z[ct][4 * g4], Z[ct][4 * g4 + 1], Z[ct][4 * g4 + 2], Z[ct][4 * g4 + 3]};
@@ -279,7 +319,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k
   // weight of the state outside the chunk
   uint4 R[4][2][NT], gf[DT][2][NT];
   __syncthreads();
-  stage_rows<TG, DK, NT>(vals, p0, cnt, d, vl);
+  stage_rows<TG, DK, NT>(vals, vl);
   __syncthreads();
 #pragma unroll
   for (int ct = 0; ct < DT; ++ct)
@@ -315,52 +355,31 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k
 #pragma unroll
   for (int t = 0; t < DT; ++t) Y[t] = zero16();
   float psum = 0.f;
+  // the state with rows l and the columns in the slots, and W with rows c and features in them
+  StateTile<DT, NT, true> state(old, pre, wold, d, a.Mp);
+  TurnedTile<DT, NT, ELU> tt;
+  wt.fetch(W, 0);
+  state.fetch(0);
+  tt.fetch(W, 0);
+#pragma unroll 1
   for (int f0 = 0; f0 < a.Mp; f0 += 32) {
-    __syncthreads();
-    stage_weights<DK, NW, ELU>(W, f0, a.M, d, wl);
-    // the state with rows l and the columns in the slots, and W with rows c and features in them
-    for (int e = threadIdx.x; e < 32 * DK * 2; e += 256) {
-      const int l = e & 31, half = (e >> 5) & 1, ks = e >> 6;
-      floatx16 x;
-#pragma unroll
-      for (int t = 0; t < 8; ++t) {
-        const int c = 16 * ks + 8 * (t >> 2) + 4 * half + (t & 3);
-        const size_t p = static_cast<size_t>(min(c, d)) * a.Mp + f0 + l;
-        x[t] = c < d ? wold * old[p] + (pre ? pre[p] : 0.f) : 0.f;
-      }
-      uint4 t[NT];
-      pack_half<NT>(x, 0, t);
-#pragma unroll
-      for (int s = 0; s < NT; ++s) sl[(ks * NT + s) * kFragLanes + 32 * half + l] = t[s];
-    }
-    for (int e = threadIdx.x; e < 32 * DT * 4; e += 256) {
-      const int c = e % (32 * DT), half = (e / (32 * DT)) & 1, k2 = e / (64 * DT);
-      floatx16 x;
-#pragma unroll
-      for (int t = 0; t < 8; ++t) {
-        const int l = f0 + 16 * k2 + 8 * (t >> 2) + 4 * half + (t & 3);
-        if constexpr (ELU)
-          x[t] = l == c ? 1.f : 0.f;
-        else
-          x[t] = l < a.M && c < d ? W[static_cast<size_t>(l) * d + c] : 0.f;
-      }
-      uint4 t[NT];
-      pack_half<NT>(x, 0, t);
-#pragma unroll
-      for (int s = 0; s < NT; ++s) tl[(((c >> 5) * 2 + k2) * NT + s) * kFragLanes + 32 * half + (c & 31)] = t[s];
-    }
-    if (threadIdx.x < 32) {
-      const size_t at = static_cast<size_t>(d) * a.Mp + f0 + threadIdx.x;
-      sden[threadIdx.x] = wold * old[at] + (pre ? pre[at] : 0.f);
+    __syncthreads();  // the operands before consumed
+    wt.put(wl);
+    if (state.any()) state.put(sl, sden);
+    tt.put(tl);
+    if (f0 + 32 < a.Mp) {
+      wt.fetch(W, f0 + 32);
+      state.fetch(f0 + 32);
+      tt.fetch(W, f0 + 32);
     }
     __syncthreads();
     floatx16 acc, lo, ph, df = zero16();
     // features of the other rows with the positions along the registers: their factors by lane
-    project_terms<DK, NSX, NW, true>(wl, tf, acc, lo);
+    project_terms<DK, NSX, NW, true, WHOLE>(weights, tf, acc, lo);
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
       const int from = 8 * (e >> 2) + 4 * lh + (e & 3);  // the lane that holds this row's factors
-      ph[e] = feature<ELU>(acc[e], lo[e], __shfl(ft.r, from), __shfl(ft.c, from), __shfl(ft.f, from));
+      ph[e] = feature<ELU, WHOLE>(acc[e], WHOLE ? lo[e] : 0.f, __shfl(ft.r, from), __shfl(ft.c, from), __shfl(ft.f, from));
     }
     if (f0 + lr >= a.M) ph = zero16();
 #pragma unroll
@@ -370,18 +389,21 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k
 #pragma unroll
       for (int s = 0; s < NT; ++s) kl[((wave * 2 + k2) * NT + s) * kFragLanes + lane] = t[s];
     }
+    if (state.any()) {
 #pragma unroll
-    for (int ks = 0; ks < DK; ++ks) {
-      uint4 f[NT];
-      read_terms<NT>(sl + ks * NT * kFragLanes, f);
-      df = mfma_terms<NT, NT>(f, gf[ks >> 1][ks & 1], df);
+      for (int ks = 0; ks < DK; ++ks) {
+        uint4 f[NT];
+        read_terms<NT>(sl + ks * NT * kFragLanes, f);
+        df = mfma_terms<NT, NT>(f, gf[ks >> 1][ks & 1], df);
+      }
+#pragma unroll
+      for (int e = 0; e < 16; ++e) df[e] = fmaf(sden[8 * (e >> 2) + 4 * lh + (e & 3)], one, df[e]);
     }
-    project_terms<DK, NSX, NW, false>(wl, of, acc, lo);
+    project_terms<DK, NSX, NW, false, WHOLE>(weights, of, acc, lo);
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
       const int l = 8 * (e >> 2) + 4 * lh + (e & 3);
-      df[e] = fmaf(sden[l], one, df[e]);
-      ph[e] = feature<ELU>(acc[e], lo[e], fo.r, fo.c, fo.f);
+      ph[e] = feature<ELU, WHOLE>(acc[e], WHOLE ? lo[e] : 0.f, fo.r, fo.c, fo.f);
       if constexpr (ELU) ph[e] = fminf(ph[e], 1.f);  // the slope of elu + 1 is e^x below zero, 1 above
       if (f0 + l >= a.M) ph[e] = 0.f;
     }
@@ -411,8 +433,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k
     }
   }
   psum += __shfl_xor(psum, 32);
-  TX* __restrict__ out = static_cast<TX*>(SIDE == 0 ? a.dq : a.dk) + base + row;
-  store_row_gradient<TX, DT, ELU>(own, Y, psum, out, i < cnt, d, a.nprf);
+  TX* __restrict__ out = static_cast<TX*>(SIDE == 0 ? a.dq : a.dk) + from + static_cast<size_t>(i) * d;
+  store_row_gradient<TX, DT, ELU>(own, own.at(i), Y, psum, out, i < cnt, a.nprf);
 }
 
 namespace {
@@ -429,9 +451,10 @@ hipError_t go(const DecayArgs& a, hipStream_t st) {
                               hipFuncAttributeMaxDynamicSharedMemorySize, lds);
   }
   const dim3 grid(static_cast<unsigned>(a.B) * a.H * a.nchunk), block(256);
-  launch_decay_states<TX, TX, DK, NT, NV, ELU, false>(a, st);
+  const bool sums = a.nchunk > 1;  // (a single chunk has no state outside it)
+  if (sums) launch_decay_states<TX, TX, DK, NT, NV, ELU, Sums::kForth>(a, st);
   hipLaunchKernelGGL((k_decay_grad<TX, DK, NT, 0, ELU>), grid, block, lds, st, a);
-  launch_decay_states<TX, float, DK, NT, NT, ELU, true>(a, st);
+  if (sums) launch_decay_states<TX, float, DK, NT, NT, ELU, Sums::kBack>(a, st);
   hipLaunchKernelGGL((k_decay_grad<TX, DK, NT, 1, ELU>), grid, block, lds, st, a);
   return hipGetLastError();
 }

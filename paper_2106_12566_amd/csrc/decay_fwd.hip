@@ -13,11 +13,13 @@ namespace krpe {
 // its rows' phi(k) to LDS as fragments, phi(q) in registers; S^T[j][i] += phi(k)
 // phi(q) for the row tiles j up to its own and the numerators' share of the
 // state, A phi(q).  Then P = S e^{-rate (i - j)} leaves its registers as the
-// operand of sum_j v_j P_ij.
+// operand of sum_j v_j P_ij.  W and the state of the next features are fetched
+// while those at hand are worked on.
 // NT: terms of features and values; NP: of P and the state.
 template <typename TX, int DK, int NT, int NP, bool ELU>
-__global__ __launch_bounds__(256) void k_decay_out(DecayArgs a) {
-  constexpr int NSX = kTermsX<TX>, DT = DK / 2, NW = NT == 1 ? 2 : 3;
+__global__ __launch_bounds__(256, sizeof(TX) == 2 && DK <= 4 ? 2 : 1) void k_decay_out(DecayArgs a) {
+  constexpr bool WHOLE = sizeof(TX) == 4;
+  constexpr int NSX = kTermsX<TX>, DT = DK / 2, NW = WHOLE ? 3 : 2;
   extern __shared__ __align__(16) uint4 smem[];
   uint4* const wl = smem;                            // [DK][NW][64]
   uint4* const sl = wl + DK * NW * kFragLanes;       // [DT][2][NP][64]
@@ -33,17 +35,32 @@ __global__ __launch_bounds__(256) void k_decay_out(DecayArgs a) {
   const int slot = a.state ? slot_of(a.slots, b, a.B, a.nslots) : kStateNone;
   const size_t base = static_cast<size_t>(bh) * a.n * d, cells = static_cast<size_t>(d + 1) * a.Mp;
   const float rl = rate_log2(a.rate[h]);
+  const Rows<float> W(a.W + static_cast<size_t>(h) * a.M * d, a.M, d);
   const int seg = ch / a.segc, inseg = ch - seg * a.segc;
-  const float* __restrict__ pre = inseg ? a.pre + (static_cast<size_t>(bh) * a.nchunk + ch) * cells : nullptr;
-  const float* __restrict__ old = a.tot ? a.tot + (static_cast<size_t>(bh) * a.nseg + seg) * cells : nullptr;
-  const float wold = decay(rl, inseg * kChunk);
+  const bool whole = a.nseg == 1;
+  const float* __restrict__ pre =
+      inseg || (whole && slot >= 0 && !a.fresh) ? a.pre + (static_cast<size_t>(bh) * a.nchunk + ch) * cells : nullptr;
+  const float* __restrict__ old = whole ? nullptr : a.tot + (static_cast<size_t>(bh) * a.nseg + seg) * cells;
+  StateTile<DT, NP, false> state(old, pre, decay(rl, inseg * kChunk), d, a.Mp);
+  const bool has = state.any();
   const int i = 32 * wave + lr;
-  const size_t row = static_cast<size_t>(p0 + min(i, cnt - 1)) * d;
+  const size_t from = base + static_cast<size_t>(p0) * d;
+  const Rows<TX> qr(static_cast<const TX*>(a.q) + from, cnt, d), kr(static_cast<const TX*>(a.k) + from, cnt, d),
+      vr(static_cast<const TX*>(a.v) + from, cnt, d);
+  WeightTile<DK, NW, ELU> wt;
+  wt.fetch(W, 0);
+  state.fetch(0);
   uint4 qf[DK][NSX], kf[DK][NSX];
-  const RowFactors fq = row_factors<ELU>(load_x<TX, DK>(static_cast<const TX*>(a.q) + base + row, i < cnt, d, qf), a.nprf,
-                                         a.log2_m);
-  const RowFactors fk = row_factors<ELU>(load_x<TX, DK>(static_cast<const TX*>(a.k) + base + row, i < cnt, d, kf), a.nprf,
-                                         a.log2_m);
+  RowFactors fq, fk;
+  {
+    Raw8<TX> x[DK], y[DK];
+    fetch_row<TX, DK>(qr, qr.at(i), x);
+    fetch_row<TX, DK>(kr, kr.at(i), y);
+    fq = row_factors<ELU>(row_square<TX, DK>(x), a.nprf, a.log2_m);
+    fk = row_factors<ELU>(row_square<TX, DK>(y), a.nprf, a.log2_m);
+#pragma unroll
+    for (int ks = 0; ks < DK; ++ks) x[ks].terms(qf[ks]), y[ks].terms(kf[ks]);
+  }
   floatx16 S[4], Z[DT];
 #pragma unroll
   for (int t = 0; t < 4; ++t) S[t] = zero16();
@@ -51,46 +68,30 @@ __global__ __launch_bounds__(256) void k_decay_out(DecayArgs a) {
   for (int t = 0; t < DT; ++t) Z[t] = zero16();
   float den = 0.f;
   if (threadIdx.x == 0) odd = 0;
+  auto weights = [&](int ks, uint4(&w)[NW]) { read_terms<NW>(wl + ks * NW * kFragLanes, w); };
+#pragma unroll 1
   for (int f0 = 0; f0 < a.Mp; f0 += 32) {
-    __syncthreads();  // the previous features consumed
-    stage_weights<DK, NW, ELU>(a.W + static_cast<size_t>(h) * a.M * d, f0, a.M, d, wl);
-    if (old) {
-      // the state before the chunk as operands: rows c, features in the slots' order
-      for (int e = threadIdx.x; e < DT * 32 * 4; e += 256) {
-        const int c = e >> 2, ks = (e >> 1) & 1, half = e & 1;
-        floatx16 x = zero16();  // (eight used)
-        if (c < d) {
-          const size_t at = static_cast<size_t>(c) * a.Mp + f0 + 16 * ks + 4 * half;
-          const float4 u = *reinterpret_cast<const float4*>(old + at), w = *reinterpret_cast<const float4*>(old + at + 8);
-          x[0] = wold * u.x, x[1] = wold * u.y, x[2] = wold * u.z, x[3] = wold * u.w;
-          x[4] = wold * w.x, x[5] = wold * w.y, x[6] = wold * w.z, x[7] = wold * w.w;
-          if (pre) {
-            const float4 y = *reinterpret_cast<const float4*>(pre + at), t = *reinterpret_cast<const float4*>(pre + at + 8);
-            x[0] += y.x, x[1] += y.y, x[2] += y.z, x[3] += y.w;
-            x[4] += t.x, x[5] += t.y, x[6] += t.z, x[7] += t.w;
-          }
-        }
-        uint4 t[NP];
-        pack_half<NP>(x, 0, t);
-#pragma unroll
-        for (int s = 0; s < NP; ++s) sl[(((c >> 5) * 2 + ks) * NP + s) * kFragLanes + 32 * half + (c & 31)] = t[s];
-      }
-      if (threadIdx.x < 32) {
-        const size_t at = static_cast<size_t>(d) * a.Mp + f0 + threadIdx.x;
-        sden[threadIdx.x] = wold * old[at] + (pre ? pre[at] : 0.f);
-      }
+    // (the waves have all read the operands before: they have passed the barrier after phi)
+    wt.put(wl);
+    if (has) state.put(sl, sden);
+    if (f0 + 32 < a.Mp) {
+      wt.fetch(W, f0 + 32);
+      state.fetch(f0 + 32);
     }
     __syncthreads();
     floatx16 acc, lo, ph;
-    project_terms<DK, NSX, NW, false>(wl, kf, acc, lo);
-#pragma unroll
-    for (int e = 0; e < 16; ++e) ph[e] = feature<ELU>(acc[e], lo[e], fk.r, fk.c, fk.f);
     const bool part = f0 + 32 > a.M;  // uniform: features past M weigh nothing
-    if (part) {
+    auto features = [&](const uint4(&xf)[DK][NSX], const RowFactors& o) {
+      project_terms<DK, NSX, NW, false, WHOLE>(weights, xf, acc, lo);
 #pragma unroll
-      for (int e = 0; e < 16; ++e)
-        if (f0 + 8 * (e >> 2) + 4 * lh + (e & 3) >= a.M) ph[e] = 0.f;
-    }
+      for (int e = 0; e < 16; ++e) ph[e] = feature<ELU, WHOLE>(acc[e], WHOLE ? lo[e] : 0.f, o.r, o.c, o.f);
+      if (part) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (f0 + 8 * (e >> 2) + 4 * lh + (e & 3) >= a.M) ph[e] = 0.f;
+      }
+    };
+    features(kf, fk);
 #pragma unroll
     for (int k2 = 0; k2 < 2; ++k2) {
       uint4 t[NT];
@@ -98,18 +99,11 @@ __global__ __launch_bounds__(256) void k_decay_out(DecayArgs a) {
 #pragma unroll
       for (int s = 0; s < NT; ++s) kl[((wave * 2 + k2) * NT + s) * kFragLanes + lane] = t[s];
     }
-    project_terms<DK, NSX, NW, false>(wl, qf, acc, lo);
-#pragma unroll
-    for (int e = 0; e < 16; ++e) ph[e] = feature<ELU>(acc[e], lo[e], fq.r, fq.c, fq.f);
-    if (part) {
-#pragma unroll
-      for (int e = 0; e < 16; ++e)
-        if (f0 + 8 * (e >> 2) + 4 * lh + (e & 3) >= a.M) ph[e] = 0.f;
-    }
+    features(qf, fq);
     uint4 pq[2][NT];
     pack_half<NT>(ph, 0, pq[0]);
     pack_half<NT>(ph, 1, pq[1]);
-    if (old) {
+    if (has) {
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         const float4 s4 = *reinterpret_cast<const float4*>(sden + 8 * g + 4 * lh);
@@ -144,9 +138,8 @@ __global__ __launch_bounds__(256) void k_decay_out(DecayArgs a) {
   for (int ct = 0; ct < DT; ++ct)
 #pragma unroll
     for (int e = 0; e < 16; ++e) Z[ct][e] *= since;
-  const TX* __restrict__ v = static_cast<const TX*>(a.v) + base;
   __syncthreads();
-  stage_columns<TX, DT, NT, Values::kClean>(v, p0, cnt, d, 4, vl, &odd);
+  stage_columns<TX, DT, 4, NT, Values::kClean>(vr, vl, &odd);
   __syncthreads();
 #pragma unroll
   for (int jt = 0; jt < 4; ++jt)
@@ -174,7 +167,7 @@ __global__ __launch_bounds__(256) void k_decay_out(DecayArgs a) {
     // values that are not finite (they went in as zeros): NaN for the rows that see them.
     // The same product over marks, 1 for such a value and 1 for a position that is seen.
     __syncthreads();
-    stage_columns<TX, DT, 1, Values::kMark>(v, p0, cnt, d, 4, vl, nullptr);
+    stage_columns<TX, DT, 4, 1, Values::kMark>(vr, vl, nullptr);
     __syncthreads();
     for (int jt = 0; jt <= wave; ++jt)
 #pragma unroll
@@ -196,7 +189,7 @@ __global__ __launch_bounds__(256) void k_decay_out(DecayArgs a) {
   }
   if (i >= cnt) return;
   using TZ = TX;
-  TZ* __restrict__ z = static_cast<TZ*>(a.z) + base + row;
+  TZ* __restrict__ z = static_cast<TZ*>(a.z) + from + static_cast<size_t>(i) * d;
   const float inv = slot == kStateBad ? NAN : 1.f / den;
 #pragma unroll
   for (int ct = 0; ct < DT; ++ct)
@@ -213,7 +206,8 @@ template <typename TX, int DK, bool ELU>
 hipError_t go(const DecayArgs& a, hipStream_t st) {
   constexpr int NT = sizeof(TX) == 2 ? 1 : 3, NP = sizeof(TX) == 2 ? 2 : 3, DT = DK / 2;
   const int BH = a.B * a.H;
-  if (a.tot) launch_decay_states<TX, TX, DK, 3, NT, ELU, false>(a, st);
+  // (a single chunk from zeros whose state is not kept needs no sums)
+  if (a.state || a.nchunk > 1) launch_decay_states<TX, TX, DK, 3, NT, ELU, Sums::kForth>(a, st);
   if (a.nchunk > 0) {
     constexpr int NW = NT == 1 ? 2 : 3;
     constexpr int feat = DK * NW + DT * 2 * NP + 8 * NT, vals = 8 * DT * NT;
@@ -233,6 +227,25 @@ hipError_t by_width(const DecayArgs& a, hipStream_t st) {
 }
 
 }  // namespace
+
+hipError_t launch_decay_commit(bool bf16, bool elu, const DecayArgs& a, hipStream_t st) {
+  auto go = [&](auto x, auto e) {
+    using TX = decltype(x);
+    constexpr int NV = sizeof(TX) == 2 ? 1 : 3;
+    constexpr bool ELU = decltype(e)::value;
+    if (a.d <= 32)
+      launch_decay_states<TX, TX, 2, 3, NV, ELU, Sums::kPath>(a, st);
+    else if (a.d <= 64)
+      launch_decay_states<TX, TX, 4, 3, NV, ELU, Sums::kPath>(a, st);
+    else
+      launch_decay_states<TX, TX, 8, 3, NV, ELU, Sums::kPath>(a, st);
+  };
+  if (bf16)
+    elu ? go(uint16_t{}, std::true_type{}) : go(uint16_t{}, std::false_type{});
+  else
+    elu ? go(float{}, std::true_type{}) : go(float{}, std::false_type{});
+  return hipGetLastError();
+}
 
 hipError_t launch_decay_fwd(bool bf16, bool elu, const DecayArgs& a, hipStream_t st) {
   if (bf16) return elu ? by_width<uint16_t, true>(a, st) : by_width<uint16_t, false>(a, st);

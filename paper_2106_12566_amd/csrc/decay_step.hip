@@ -1,6 +1,5 @@
-// Single tokens (krpe_decay_step), the accepted tokens of a drafted tree
-// (krpe_decay_commit) and copies within a pool of states (krpe_state_copy).
-// All three are bound by the states' bytes.
+// Single tokens (krpe_decay_step) and copies within a pool of states
+// (krpe_decay_state_copy), both bound by the states' bytes.
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
@@ -147,59 +146,6 @@ __global__ __launch_bounds__(256) void k_decay_step(PoolArgs a) {
   }
 }
 
-// The tokens tree[b][0 .. n) of a sequence, up to the first that is none of its T, taken into
-// its state: A <- e^{-rate n} A + sum_i e^{-rate (n - 1 - i)} [v; 1] phi(k)^T, eight at a time.
-template <typename TX, bool ELU>
-__global__ __launch_bounds__(256) void k_decay_commit(PoolArgs a) {
-  constexpr int R = 8;
-  extern __shared__ __align__(16) float sm[];
-  const int d = a.d, M = a.M, M4 = (M + 3) & ~3, d4 = (d + 3) & ~3;
-  float *x = sm, *f = sm + R * d4, *v = f + R * M4;  // v: [R][d + 1]
-  __shared__ float sq[R];
-  const int b = blockIdx.x / a.H, h = blockIdx.x % a.H;
-  const int slot = slot_of(a.slots, b, a.B, a.nslots);
-  const int* __restrict__ path = a.tree + static_cast<size_t>(b) * a.P;
-  int n = 0;
-  while (n < a.P && path[n] >= 0 && path[n] < a.T) ++n;
-  if (slot < 0 || n == 0) return;
-  const float rl = rate_log2(a.rate[h]);
-  const bool vec = M % 4 == 0;
-  const int L = lanes_of(M4), lane = threadIdx.x % L, per = 256 / L;
-  float* __restrict__ st = a.state + (static_cast<size_t>(slot) * a.H + h) * (d + 1) * M;
-  for (int i0 = 0; i0 < n; i0 += R) {
-    const int cnt = min(R, n - i0);
-    __syncthreads();
-    for (int e = threadIdx.x; e < R * d; e += 256) {
-      const int r = e / d, c = e % d;
-      const size_t at = (static_cast<size_t>(blockIdx.x) * a.T + path[i0 + min(r, cnt - 1)]) * d + c;
-      x[e] = r < cnt ? to_f32(static_cast<const TX*>(a.k)[at]) : 0.f;
-      v[r * (d + 1) + c] = r < cnt ? to_f32(static_cast<const TX*>(a.v)[at]) : 0.f;
-    }
-    if (threadIdx.x < R) v[threadIdx.x * (d + 1) + d] = static_cast<int>(threadIdx.x) < cnt ? 1.f : 0.f;
-    __syncthreads();
-    row_squares<R>(x, d, sq);
-    __syncthreads();
-    row_features<R, ELU>(x, sq, a.W + static_cast<size_t>(h) * M * d, d, M, M4, a.log_m, a.nprf, f);
-    __syncthreads();
-    float w[R];
-#pragma unroll
-    for (int r = 0; r < R; ++r) w[r] = r < cnt ? decay(rl, cnt - 1 - r) : 0.f;
-    const float w0 = decay(rl, cnt);
-    for (int c = threadIdx.x / L; c <= d; c += per)
-      for (int l = 4 * lane; l < M; l += 4 * L) {
-        float4 u = load_cells(st + static_cast<size_t>(c) * M, l, M, vec);
-        u.x *= w0, u.y *= w0, u.z *= w0, u.w *= w0;
-#pragma unroll
-        for (int r = 0; r < R; ++r) {
-          const float4 fk = *reinterpret_cast<const float4*>(f + r * M4 + l);
-          const float y = w[r] * v[r * (d + 1) + c];
-          u.x = fmaf(y, fk.x, u.x), u.y = fmaf(y, fk.y, u.y), u.z = fmaf(y, fk.z, u.z), u.w = fmaf(y, fk.w, u.w);
-        }
-        store_cells(st + static_cast<size_t>(c) * M, l, M, vec, u);
-      }
-  }
-}
-
 // state[dst[i]] = state[src[i]] for all i at once (-1: zeros).  A thread owns the same cells of
 // every slot: it reads them all before it writes any, in the moves' order, so moves may
 // overlap in any way and a slot written twice keeps the last.
@@ -230,17 +176,6 @@ hipError_t launch_decay_step(bool bf16, bool elu, const PoolArgs& a, hipStream_t
     elu ? k_decay_step<uint16_t, true><<<grid, block, lds, st>>>(a) : k_decay_step<uint16_t, false><<<grid, block, lds, st>>>(a);
   else
     elu ? k_decay_step<float, true><<<grid, block, lds, st>>>(a) : k_decay_step<float, false><<<grid, block, lds, st>>>(a);
-  return hipGetLastError();
-}
-
-hipError_t launch_decay_commit(bool bf16, bool elu, const PoolArgs& a, hipStream_t st) {
-  const int M4 = (a.M + 3) & ~3, d4 = (a.d + 3) & ~3;
-  const dim3 grid(static_cast<unsigned>(a.B) * a.H), block(256);
-  const size_t lds = (8 * d4 + 8 * M4 + 8 * (a.d + 1)) * sizeof(float);
-  if (bf16)
-    elu ? k_decay_commit<uint16_t, true><<<grid, block, lds, st>>>(a) : k_decay_commit<uint16_t, false><<<grid, block, lds, st>>>(a);
-  else
-    elu ? k_decay_commit<float, true><<<grid, block, lds, st>>>(a) : k_decay_commit<float, false><<<grid, block, lds, st>>>(a);
   return hipGetLastError();
 }
 

@@ -22,7 +22,8 @@ constexpr int kTreeWaves = 4;
 // RT: row tiles of 32 nodes (T <= 32 RT); NT: terms of features and values; NPP: of P and the state.
 template <typename TX, int DK, int NT, int NPP, int RT, bool ELU>
 __global__ __launch_bounds__(64 * kTreeWaves) void k_decay_tree(PoolArgs a) {
-  constexpr int NSX = kTermsX<TX>, DT = DK / 2, NW = NT == 1 ? 2 : 3, NP = RT == 1 ? 1 : 3;
+  constexpr bool WHOLE = sizeof(TX) == 4;
+  constexpr int NSX = kTermsX<TX>, DT = DK / 2, NW = WHOLE ? 3 : 2, NP = RT == 1 ? 1 : 3;
   // partial sums: S tiles [wave][NP], then one row tile's Z [wave][DT] at a time
   constexpr int kPart = kTreeWaves * (NP > DT ? NP : DT) * 16;
   __shared__ __align__(16) float part[kPart * 64];
@@ -37,14 +38,14 @@ __global__ __launch_bounds__(64 * kTreeWaves) void k_decay_tree(PoolArgs a) {
   const int slot = slot_of(a.slots, b, a.B, a.nslots);
   const float* __restrict__ st = slot >= 0 ? a.state + (static_cast<size_t>(slot) * a.H + h) * (d + 1) * M : nullptr;
   const size_t base = static_cast<size_t>(blockIdx.x) * T * d;
-  const TX* __restrict__ q = static_cast<const TX*>(a.q) + base;
-  const TX* __restrict__ k = static_cast<const TX*>(a.k) + base;
-  const TX* __restrict__ v = static_cast<const TX*>(a.v) + base;
+  const Rows<TX> q(static_cast<const TX*>(a.q) + base, T, d), k(static_cast<const TX*>(a.k) + base, T, d),
+      v(static_cast<const TX*>(a.v) + base, T, d);
+  const Rows<float> W(a.W + static_cast<size_t>(h) * M * d, M, d);
   const float rl = rate_log2(a.rate[h]);
   if (threadIdx.x == 0) odd = 0;
   if (wave == 0) {
     // ancestors by pointer doubling; a node without a valid parent, or below one, sees nothing
-    int up = lane < T ? a.tree[static_cast<size_t>(b) * T + lane] : -2;
+    int up = lane < T ? a.parent[static_cast<size_t>(b) * T + lane] : -2;
     bool dead = up < -1 || up >= lane;
     unsigned long long m = 1ull << lane;
     if (dead) up = -1;
@@ -61,7 +62,7 @@ __global__ __launch_bounds__(64 * kTreeWaves) void k_decay_tree(PoolArgs a) {
     if (lane < 32 * RT) seen[lane] = dead ? 0ull : m;
   }
   __syncthreads();
-  stage_columns<TX, DT, NT, Values::kClean>(v, 0, T, d, RT, vl, &odd);
+  stage_columns<TX, DT, RT, NT, Values::kClean>(v, vl, &odd);
   floatx16 S[NP], Z[RT][DT];
   float den[RT];
 #pragma unroll
@@ -75,41 +76,34 @@ __global__ __launch_bounds__(64 * kTreeWaves) void k_decay_tree(PoolArgs a) {
   const bool vec = M % 4 == 0;
   for (int f0 = 32 * wave; f0 < M; f0 += 32 * kTreeWaves) {
     uint4 wf[DK][NW];
-    const int fl = f0 + lr;
 #pragma unroll
     for (int ks = 0; ks < DK; ++ks) {
-      const int c = 16 * ks + 8 * lh;
       float v8[8];
-      if constexpr (ELU) {
-#pragma unroll
-        for (int t = 0; t < 8; ++t) v8[t] = c + t == fl ? 1.f : 0.f;
-      } else {
-        load8(a.W + (static_cast<size_t>(h) * M + min(fl, M - 1)) * d + min(c, d - 1), fl < M ? d - c : 0, d % 4 == 0, v8);
-      }
+      load_weights<ELU>(W, f0 + lr, 16 * ks + 8 * lh, v8);
       uint4 t3[3];
       split_bf16x8(v8, t3);
 #pragma unroll
       for (int s = 0; s < NW; ++s) wf[ks][s] = t3[s];
     }
     // features of a row tile (lane: row; features along the registers), zeros past M
-    auto features = [&](const TX* __restrict__ x, int r, floatx16& ph) {
+    auto features = [&](const Rows<TX>& x, int r, floatx16& ph) {
       const int i = 32 * r + lr;
+      Raw8<TX> raw[DK];
+      fetch_row<TX, DK>(x, x.at(i), raw);
+      const RowFactors o = row_factors<ELU>(row_square<TX, DK>(raw), a.nprf, a.log2_m);
       uint4 xf[DK][NSX];
-      const RowFactors o = row_factors<ELU>(load_x<TX, DK>(x + static_cast<size_t>(min(i, T - 1)) * d, i < T, d, xf), a.nprf,
-                                            a.log2_m);
-      floatx16 acc = zero16(), lo = zero16();
 #pragma unroll
-      for (int ks = 0; ks < DK; ++ks) {
+      for (int ks = 0; ks < DK; ++ks) raw[ks].terms(xf[ks]);
+      floatx16 acc, lo;
+      project_terms<DK, NSX, NW, false, WHOLE>(
+          [&](int ks, uint4(&w)[NW]) {
 #pragma unroll
-        for (int s = 2; s >= 1; --s)
-#pragma unroll
-          for (int j = 0; j <= s; ++j)
-            if (j < NW && s - j < NSX) lo = mfma_bf16(wf[ks][j], xf[ks][s - j], lo);
-        acc = mfma_bf16(wf[ks][0], xf[ks][0], acc);
-      }
+            for (int n = 0; n < NW; ++n) w[n] = wf[ks][n];
+          },
+          xf, acc, lo);
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        ph[e] = feature<ELU>(acc[e], lo[e], o.r, o.c, o.f);
+        ph[e] = feature<ELU, WHOLE>(acc[e], WHOLE ? lo[e] : 0.f, o.r, o.c, o.f);
         if (f0 + 8 * (e >> 2) + 4 * lh + (e & 3) >= M) ph[e] = 0.f;
       }
     };
@@ -245,7 +239,7 @@ __global__ __launch_bounds__(64 * kTreeWaves) void k_decay_tree(PoolArgs a) {
           const int c = 32 * ct + 8 * (e >> 2) + 4 * lh + (e & 3);
           if (c < d)
             for (int j = 0; j < T; ++j)
-              if (((m >> j) & 1) && !finite(to_f32(v[static_cast<size_t>(j) * d + c]))) o[e] = NAN;
+              if (((m >> j) & 1) && !finite(v.one(v.at(v.at(j), c)))) o[e] = NAN;
         }
       }
       if (i < T)
