@@ -147,24 +147,34 @@ __global__ __launch_bounds__(256) void k_decay_step(PoolArgs a) {
 }
 
 // state[dst[i]] = state[src[i]] for all i at once (-1: zeros).  A thread owns the same cells of
-// every slot: it reads them all before it writes any, in the moves' order, so moves may
-// overlap in any way and a slot written twice keeps the last.
-template <typename T>
-__global__ __launch_bounds__(64) void k_state_copy(T* __restrict__ state, const int* __restrict__ src,
-                                                   const int* __restrict__ dst, int count, int nslots, long long cells) {
-  extern __shared__ __align__(16) char raw[];
-  T* const kept = reinterpret_cast<T*>(raw) + threadIdx.x;  // [count][64]
-  const long long e = static_cast<long long>(blockIdx.x) * 64 + threadIdx.x;
-  if (e >= cells) return;
-  for (int i = 0; i < count; ++i) {
-    const int s = src[i];
-    T x{};
-    if (s >= 0 && s < nslots) x = state[s * cells + e];
-    kept[i * 64] = x;
+// every slot: it reads them all into registers before it writes any, in the moves' order, so
+// moves may overlap in any way and a slot written twice keeps the last.  CAP moves of a T fill
+// up to 448 of a wave's 512 registers: that many reads are in flight, and one wave per SIMD
+// fills HBM (the kept cells in LDS, read one by one: 106 us for 96 moves of 1 MiB; in registers:
+// 41 us, 5.0 TB/s, a plain copy's rate).
+template <typename T, int CAP>
+__global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(1))) void k_state_copy(
+    T* __restrict__ state, const int* __restrict__ src, const int* __restrict__ dst, int count, int nslots, long long cells) {
+  __shared__ int from[CAP], to[CAP];  // from -2: no move
+  const long long e = static_cast<long long>(xcd_block(blockIdx.x, gridDim.x)) * 64 + threadIdx.x;
+  for (int i = threadIdx.x; i < CAP; i += 64) {
+    const int s = i < count ? src[i] : -2, t = i < count ? dst[i] : -1;
+    from[i] = t >= 0 && t < nslots && s >= -1 && s < nslots ? s : -2;
+    to[i] = t;
   }
-  for (int i = 0; i < count; ++i) {
-    const int s = src[i], t = dst[i];
-    if (t >= 0 && t < nslots && s >= -1 && s < nslots) state[t * cells + e] = kept[i * 64];
+  __syncthreads();
+  const bool live = e < cells;
+  T kept[CAP];
+#pragma unroll
+  for (int i = 0; i < CAP; ++i) {
+    const int s = __builtin_amdgcn_readfirstlane(from[i]);
+    kept[i] = T{};
+    if (s >= 0 && live) kept[i] = state[s * cells + e];
+  }
+#pragma unroll
+  for (int i = 0; i < CAP; ++i) {
+    const int s = __builtin_amdgcn_readfirstlane(from[i]), t = __builtin_amdgcn_readfirstlane(to[i]);
+    if (s >= -1 && live) state[t * cells + e] = kept[i];
   }
 }
 
@@ -179,15 +189,28 @@ hipError_t launch_decay_step(bool bf16, bool elu, const PoolArgs& a, hipStream_t
   return hipGetLastError();
 }
 
+namespace {
+template <typename T, int CAP>
+void copy_cells(float* state, const int* src, const int* dst, int count, int nslots, long long cells, hipStream_t st) {
+  cells = cells * sizeof(float) / sizeof(T);
+  hipLaunchKernelGGL((k_state_copy<T, CAP>), dim3(static_cast<unsigned>((cells + 63) / 64)), dim3(64), 0, st,
+                     reinterpret_cast<T*>(state), src, dst, count, nslots, cells);
+}
+}  // namespace
+
 hipError_t launch_state_copy(float* state, const int* src, const int* dst, int count, int nslots, long long cells,
                              hipStream_t st) {
-  // 64 KiB of LDS hold the cells of a work-group: 16 bytes a thread up to 64 moves, 4 beyond
-  if (count <= 64 && cells % 4 == 0)
-    k_state_copy<float4><<<static_cast<unsigned>((cells / 4 + 63) / 64), 64, count * 1024, st>>>(
-        reinterpret_cast<float4*>(state), src, dst, count, nslots, cells / 4);
+  // the widest cells that the registers hold for so many moves
+  if (cells % 4 == 0 && count <= 16)
+    copy_cells<float4, 16>(state, src, dst, count, nslots, cells, st);
+  else if (cells % 4 == 0 && count <= 64)
+    copy_cells<float4, 64>(state, src, dst, count, nslots, cells, st);
+  else if (cells % 4 == 0 && count <= 112)
+    copy_cells<float4, 112>(state, src, dst, count, nslots, cells, st);
+  else if (cells % 2 == 0 && count <= 224)
+    copy_cells<float2, 224>(state, src, dst, count, nslots, cells, st);
   else
-    k_state_copy<float><<<static_cast<unsigned>((cells + 63) / 64), 64, count * 256, st>>>(state, src, dst, count,
-                                                                                          nslots, cells);
+    copy_cells<float, 256>(state, src, dst, count, nslots, cells, st);
   return hipGetLastError();
 }
 

@@ -5,10 +5,11 @@
 //   num_t | den_t = e^{-rate (dep_t + 1)} A phi(q_t)
 //                 + sum_{a in anc(t)} e^{-rate (dep_t - dep_a)} (phi(q_t) . phi(k_a)) [v_a | 1]
 //
-// A work-group is one sequence and head.  Its waves split the features (the
-// state is read once, straight into operands, by the wave whose features they
-// are), so S = phi(K) phi(Q)^T and A phi(Q) leave the waves as partial sums,
-// which are added through LDS in a fixed order.
+// A work-group is one sequence and head.  Four waves for each row tile of 32
+// nodes split the features; what a wave needs of the state goes straight from
+// memory into its operands, asked for before any row is worked on.  S = phi(K)
+// phi(Q)^T and A phi(Q) leave the waves as partial sums, which are added
+// through LDS in a fixed order.
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
@@ -17,33 +18,87 @@
 
 namespace krpe {
 
-constexpr int kTreeWaves = 4;
+constexpr int kSplit = 4;  // waves of a row tile
 
-// RT: row tiles of 32 nodes (T <= 32 RT); NT: terms of features and values; NPP: of P and the state.
+// RT: row tiles (T <= 32 RT); NT: terms of features and values; NPP: of P and the state.
 template <typename TX, int DK, int NT, int NPP, int RT, bool ELU>
-__global__ __launch_bounds__(64 * kTreeWaves) void k_decay_tree(PoolArgs a) {
+__global__ __launch_bounds__(64 * kSplit * RT, sizeof(TX) == 2 && DK <= 4 ? 2 : 1) void k_decay_tree(PoolArgs a) {
   constexpr bool WHOLE = sizeof(TX) == 4;
+  constexpr int THREADS = 64 * kSplit * RT, NX = sizeof(TX) / 2;
   constexpr int NSX = kTermsX<TX>, DT = DK / 2, NW = WHOLE ? 3 : 2, NP = RT == 1 ? 1 : 3;
-  // partial sums: S tiles [wave][NP], then one row tile's Z [wave][DT] at a time
-  constexpr int kPart = kTreeWaves * (NP > DT ? NP : DT) * 16;
-  __shared__ __align__(16) float part[kPart * 64];
-  __shared__ __align__(16) uint4 pl[NP][2][NPP][64];      // P as operands
+  constexpr int CG = DT < 2 ? DT : 2;  // column tiles summed at a time
+  // first the rows as they are [k, q][RT][DK][NX][64]; then the partial sums: S tiles [kSplit][NP], Z
+  // [kSplit][RT][CG] a group of columns at a time
+  constexpr int kRowsX = 2 * RT * DK * NX * 64, kTiles = NP > RT * CG ? NP : RT * CG, kPart = kSplit * kTiles * 16 * 16;
+  __shared__ __align__(16) uint4 area[kRowsX > kPart ? kRowsX : kPart];
+  uint4* const xl = area;
+  float* const part = reinterpret_cast<float*>(area);
+  __shared__ __align__(16) uint4 pl[NP][2][NPP][64];  // P as operands
   __shared__ __align__(16) uint4 vl[RT * DT * 2 * NT * 64];
-  __shared__ float dpart[kTreeWaves][32 * RT], dsum[NP][32];
+  __shared__ float dpart[kSplit][32 * RT], dsum[NP][32];
+  __shared__ float fr[2][32 * RT], fc[2][32 * RT], ff[2][32 * RT];
   __shared__ unsigned long long seen[32 * RT];
   __shared__ int odd;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int lr = lane & 31, lh = lane >> 5;
+  const int lr = lane & 31, lh = lane >> 5, fw = wave % kSplit, r = wave / kSplit;
   const int b = blockIdx.x / a.H, h = blockIdx.x % a.H, d = a.d, T = a.T, M = a.M;
-  const int slot = slot_of(a.slots, b, a.B, a.nslots);
-  const float* __restrict__ st = slot >= 0 ? a.state + (static_cast<size_t>(slot) * a.H + h) * (d + 1) * M : nullptr;
   const size_t base = static_cast<size_t>(blockIdx.x) * T * d;
   const Rows<TX> q(static_cast<const TX*>(a.q) + base, T, d), k(static_cast<const TX*>(a.k) + base, T, d),
       v(static_cast<const TX*>(a.v) + base, T, d);
   const Rows<float> W(a.W + static_cast<size_t>(h) * M * d, M, d);
+  Raw8<TX> raw[DK];  // waves 0 .. 2 RT - 1: a row tile of k (even) or q
+  const bool stages = wave < 2 * RT;
+  if (stages) fetch_row<TX, DK>(wave & 1 ? q : k, v.at(32 * (wave >> 1) + lr), raw);
+  ColumnTile<TX, DT, RT, THREADS> cols;
+  cols.fetch(v, [&](int x) { return v.at(x); });
+  float w8[DK][8];
+  auto fetch_weights = [&](int f0) {
+#pragma unroll
+    for (int ks = 0; ks < DK; ++ks) load_weights<ELU>(W, f0 + lr, 16 * ks + 8 * lh, w8[ks]);
+  };
+  const int slot = slot_of(a.slots, b, a.B, a.nslots);
+  const float* __restrict__ st = slot >= 0 ? a.state + (static_cast<size_t>(slot) * a.H + h) * (d + 1) * M : nullptr;
+  const Rows<float> sr(st ? st : a.state, st ? d + 1 : 0, M);  // (no state: zeros)
+  const bool vec = M % 4 == 0;
+  // (a column tile's share is asked for when the one before is used where registers are short)
+  constexpr bool LATE = DK == 8 || (WHOLE && DK == 4);
+  float s8[LATE ? 1 : DT][2][8], sd[16];
+  auto fetch_state = [&](int f0, int ct, float(&s)[2][8]) {
+#pragma unroll
+    for (int k2 = 0; k2 < 2; ++k2) {
+      const int c = 32 * ct + lr, l = f0 + 16 * k2 + 4 * lh;
+      const uint32_t o = sr.at(c);
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        if (vec) {
+          const uint4 u = sr.b128(c < d && l + 8 * x < M ? o + 4u * (l + 8 * x) : kOut);
+          s[k2][4 * x] = __uint_as_float(u.x), s[k2][4 * x + 1] = __uint_as_float(u.y);
+          s[k2][4 * x + 2] = __uint_as_float(u.z), s[k2][4 * x + 3] = __uint_as_float(u.w);
+        } else {
+#pragma unroll
+          for (int t = 0; t < 4; ++t)
+            s[k2][4 * x + t] = sr.one(c < d && l + 8 * x + t < M ? o + 4u * (l + 8 * x + t) : kOut);
+        }
+      }
+    }
+  };
+  auto fetch_last = [&](int f0) {
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const int l = f0 + 8 * g + 4 * lh;
+      if (vec) {
+        const uint4 u = sr.b128(l < M ? sr.at(d) + 4u * l : kOut);
+        sd[4 * g] = __uint_as_float(u.x), sd[4 * g + 1] = __uint_as_float(u.y);
+        sd[4 * g + 2] = __uint_as_float(u.z), sd[4 * g + 3] = __uint_as_float(u.w);
+      } else {
+#pragma unroll
+        for (int t = 0; t < 4; ++t) sd[4 * g + t] = sr.one(l + t < M ? sr.at(d) + 4u * (l + t) : kOut);
+      }
+    }
+  };
   const float rl = rate_log2(a.rate[h]);
   if (threadIdx.x == 0) odd = 0;
-  if (wave == 0) {
+  if (wave == kSplit * RT - 1) {
     // ancestors by pointer doubling; a node without a valid parent, or below one, sees nothing
     int up = lane < T ? a.parent[static_cast<size_t>(b) * T + lane] : -2;
     bool dead = up < -1 || up >= lane;
@@ -61,118 +116,111 @@ __global__ __launch_bounds__(64 * kTreeWaves) void k_decay_tree(PoolArgs a) {
     }
     if (lane < 32 * RT) seen[lane] = dead ? 0ull : m;
   }
-  __syncthreads();
-  stage_columns<TX, DT, RT, NT, Values::kClean>(v, vl, &odd);
-  floatx16 S[NP], Z[RT][DT];
-  float den[RT];
+  floatx16 S[RT], Z[DT];  // S: (key tile 0 and, in row tile 1, key tile 1)
+  float den = 0.f;
 #pragma unroll
-  for (int t = 0; t < NP; ++t) S[t] = zero16();
+  for (int t = 0; t < RT; ++t) S[t] = zero16();
 #pragma unroll
-  for (int r = 0; r < RT; ++r) {
-    den[r] = 0.f;
+  for (int t = 0; t < DT; ++t) Z[t] = zero16();
+  int f0 = 32 * fw;
+#pragma unroll 1
+  do {  // (a wave without features has zeros)
+    fetch_weights(f0);
+    if constexpr (!LATE) {
 #pragma unroll
-    for (int t = 0; t < DT; ++t) Z[r][t] = zero16();
-  }
-  const bool vec = M % 4 == 0;
-  for (int f0 = 32 * wave; f0 < M; f0 += 32 * kTreeWaves) {
+      for (int ct = 0; ct < DT; ++ct) fetch_state(f0, ct, s8[ct]);
+    }
+    fetch_last(f0);
+    if (f0 < 32 * kSplit) {  // the first time
+      if (stages) {
+        const RowFactors o = row_factors<ELU>(row_square<TX, DK>(raw), a.nprf, a.log2_m);
+        const int w = wave & 1, t = wave >> 1;
+        if (lh == 0) fr[w][32 * t + lr] = o.r, fc[w][32 * t + lr] = o.c, ff[w][32 * t + lr] = o.f;
+#pragma unroll
+        for (int ks = 0; ks < DK; ++ks)
+#pragma unroll
+          for (int n = 0; n < NX; ++n) xl[(((w * RT + t) * DK + ks) * NX + n) * 64 + lane] = raw[ks].u[n];
+      }
+      __syncthreads();  // (odd is clear)
+      cols.template put<NT, Values::kClean>(vl, &odd);
+    }
     uint4 wf[DK][NW];
 #pragma unroll
     for (int ks = 0; ks < DK; ++ks) {
-      float v8[8];
-      load_weights<ELU>(W, f0 + lr, 16 * ks + 8 * lh, v8);
       uint4 t3[3];
-      split_bf16x8(v8, t3);
+      split_bf16x8(w8[ks], t3);
 #pragma unroll
       for (int s = 0; s < NW; ++s) wf[ks][s] = t3[s];
     }
     // features of a row tile (lane: row; features along the registers), zeros past M
-    auto features = [&](const Rows<TX>& x, int r, floatx16& ph) {
-      const int i = 32 * r + lr;
-      Raw8<TX> raw[DK];
-      fetch_row<TX, DK>(x, x.at(i), raw);
-      const RowFactors o = row_factors<ELU>(row_square<TX, DK>(raw), a.nprf, a.log2_m);
+    auto features = [&](int w, int t, floatx16& ph, uint4(&p)[2][NT]) {
       uint4 xf[DK][NSX];
 #pragma unroll
-      for (int ks = 0; ks < DK; ++ks) raw[ks].terms(xf[ks]);
+      for (int ks = 0; ks < DK; ++ks) {
+        Raw8<TX> x;
+        read_terms<NX>(xl + ((w * RT + t) * DK + ks) * NX * 64, x.u);
+        x.terms(xf[ks]);
+      }
       floatx16 acc, lo;
       project_terms<DK, NSX, NW, false, WHOLE>(
-          [&](int ks, uint4(&w)[NW]) {
+          [&](int ks, uint4(&y)[NW]) {
 #pragma unroll
-            for (int n = 0; n < NW; ++n) w[n] = wf[ks][n];
+            for (int n = 0; n < NW; ++n) y[n] = wf[ks][n];
           },
           xf, acc, lo);
+      const float r_ = fr[w][32 * t + lr], c_ = fc[w][32 * t + lr], f_ = ff[w][32 * t + lr];
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        ph[e] = feature<ELU, WHOLE>(acc[e], WHOLE ? lo[e] : 0.f, o.r, o.c, o.f);
+        ph[e] = feature<ELU, WHOLE>(acc[e], WHOLE ? lo[e] : 0.f, r_, c_, f_);
         if (f0 + 8 * (e >> 2) + 4 * lh + (e & 3) >= M) ph[e] = 0.f;
       }
+      pack_half<NT>(ph, 0, p[0]);
+      pack_half<NT>(ph, 1, p[1]);
     };
-    uint4 pk[RT][2][NT], pq[RT][2][NT];
+    uint4 pk[2][NT], pq[2][NT];
+    floatx16 ph;
+    features(1, r, ph, pq);
 #pragma unroll
-    for (int r = 0; r < RT; ++r) {
-      floatx16 ph;
-      features(k, r, ph);
-      pack_half<NT>(ph, 0, pk[r][0]);
-      pack_half<NT>(ph, 1, pk[r][1]);
-      features(q, r, ph);
-      pack_half<NT>(ph, 0, pq[r][0]);
-      pack_half<NT>(ph, 1, pq[r][1]);
-      if (st) {
-        const float* __restrict__ sd = st + static_cast<size_t>(d) * M;
+    for (int e = 0; e < 16; ++e) den = fmaf(ph[e], sd[e], den);
 #pragma unroll
-        for (int e = 0; e < 16; ++e) den[r] = fmaf(ph[e], sd[min(f0 + 8 * (e >> 2) + 4 * lh + (e & 3), M - 1)], den[r]);
+    for (int ct = 0; ct < DT; ++ct) {
+      if constexpr (LATE) fetch_state(f0, ct, s8[0]);
+#pragma unroll
+      for (int k2 = 0; k2 < 2; ++k2) {
+        const float(&x)[8] = s8[LATE ? 0 : ct][k2];
+        uint32_t p[4][NPP];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) split_pair<NPP>(x[2 * j], x[2 * j + 1], p[j]);
+        uint4 t[NPP];
+#pragma unroll
+        for (int s = 0; s < NPP; ++s) t[s] = make_uint4(p[0][s], p[1][s], p[2][s], p[3][s]);
+        Z[ct] = mfma_terms<NPP, NT>(t, pq[k2], Z[ct]);
       }
     }
+    features(0, 0, ph, pk);
 #pragma unroll
-    for (int k2 = 0; k2 < 2; ++k2) {
-      S[0] = mfma_terms<NT, NT>(pk[0][k2], pq[0][k2], S[0]);
-      if constexpr (RT == 2) {
-        S[1] = mfma_terms<NT, NT>(pk[0][k2], pq[1][k2], S[1]);
-        S[2] = mfma_terms<NT, NT>(pk[1][k2], pq[1][k2], S[2]);
-      }
+    for (int k2 = 0; k2 < 2; ++k2) S[0] = mfma_terms<NT, NT>(pk[k2], pq[k2], S[0]);
+    if (RT == 2 && r == 1) {
+      features(0, 1, ph, pk);
+#pragma unroll
+      for (int k2 = 0; k2 < 2; ++k2) S[RT - 1] = mfma_terms<NT, NT>(pk[k2], pq[k2], S[RT - 1]);
     }
-    if (st) {
+    f0 += 32 * kSplit;
+  } while (f0 < M);
+  __syncthreads();  // the rows are consumed: their place takes the sums
+  // S, tile t: (row tile, key tile) = (0, 0), (1, 0), (1, 1): the waves' sums, masked and weighted, as
+  // operands
+  auto put = [&](int t, int tiles, const floatx16& x) {
 #pragma unroll
-      for (int ct = 0; ct < DT; ++ct) {
-        const int c = 32 * ct + lr;
-        const float* __restrict__ sr = st + static_cast<size_t>(min(c, d)) * M;
-#pragma unroll
-        for (int k2 = 0; k2 < 2; ++k2) {
-          floatx16 x = zero16();  // (eight used)
-          const int l = f0 + 16 * k2 + 4 * lh;
-          if (c < d) {
-            if (vec && l + 12 <= M) {
-              const float4 u = *reinterpret_cast<const float4*>(sr + l), w = *reinterpret_cast<const float4*>(sr + l + 8);
-              x[0] = u.x, x[1] = u.y, x[2] = u.z, x[3] = u.w, x[4] = w.x, x[5] = w.y, x[6] = w.z, x[7] = w.w;
-            } else {
-#pragma unroll
-              for (int t = 0; t < 8; ++t) {
-                const int at = l + (t & 3) + 8 * (t >> 2);
-                x[t] = at < M ? sr[at] : 0.f;
-              }
-            }
-          }
-          uint4 t[NPP];
-          pack_half<NPP>(x, 0, t);
-#pragma unroll
-          for (int r = 0; r < RT; ++r) Z[r][ct] = mfma_terms<NPP, NT>(t, pq[r][k2], Z[r][ct]);
-        }
-      }
-    }
-  }
-  // S: the waves' sums, masked and weighted, as operands
-#pragma unroll
-  for (int t = 0; t < NP; ++t)
-#pragma unroll
-    for (int e = 0; e < 16; ++e) part[((wave * NP + t) * 16 + e) * 64 + lane] = S[t][e];
-#pragma unroll
-  for (int r = 0; r < RT; ++r) {
-    const float s = den[r] + __shfl_xor(den[r], 32);
-    if (lh == 0) dpart[wave][32 * r + lr] = s;
-  }
+    for (int e = 0; e < 16; ++e) part[((fw * tiles + t) * 16 + e) * 64 + lane] = x[e];
+  };
+  put(r, NP, S[0]);
+  if (RT == 2 && r == 1) put(2 % NP, NP, S[RT - 1]);
+  den += __shfl_xor(den, 32);
+  if (lh == 0) dpart[fw][32 * r + lr] = den;
   __syncthreads();
-  for (int t = wave; t < NP; t += kTreeWaves) {
-    const int it = t ? 1 : 0, jt = t == 2 ? 1 : 0;  // (row tile, column tile)
+  if (wave < NP) {
+    const int t = wave, it = t ? 1 : 0, jt = t == 2 ? 1 : 0;
     const int i = 32 * it + lr;
     const unsigned long long m = seen[i];
     const int dep = __popcll(m) - 1;
@@ -183,7 +231,7 @@ __global__ __launch_bounds__(64 * kTreeWaves) void k_decay_tree(PoolArgs a) {
       const int j = 32 * jt + 8 * (e >> 2) + 4 * lh + (e & 3);
       float x = 0.f;
 #pragma unroll
-      for (int w = 0; w < kTreeWaves; ++w) x += part[((w * NP + t) * 16 + e) * 64 + lane];
+      for (int w = 0; w < kSplit; ++w) x += part[((w * NP + t) * 16 + e) * 64 + lane];
       p[e] = (m >> j) & 1 ? x * decay(rl, dep - (__popcll(seen[j]) - 1)) : 0.f;
       s += p[e];
     }
@@ -198,39 +246,43 @@ __global__ __launch_bounds__(64 * kTreeWaves) void k_decay_tree(PoolArgs a) {
     }
   }
   TX* __restrict__ z = static_cast<TX*>(a.z) + base;
+  const int i = 32 * r + lr;
+  const unsigned long long m = seen[i];
+  const float since = decay(rl, __popcll(m));
+  float inv = 0.f;
 #pragma unroll
-  for (int r = 0; r < RT; ++r) {
+  for (int g = 0; g < DT / CG; ++g) {
     __syncthreads();
 #pragma unroll
-    for (int ct = 0; ct < DT; ++ct)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) part[((wave * DT + ct) * 16 + e) * 64 + lane] = Z[r][ct][e];
+    for (int ct = 0; ct < CG; ++ct) put(r * CG + ct, RT * CG, Z[CG * g + ct]);
     __syncthreads();
-    const int i = 32 * r + lr;
-    const unsigned long long m = seen[i];
-    const float since = decay(rl, __popcll(m));
-    float dn = 0.f;
+    if (g == 0) {
+      float dn = 0.f;
 #pragma unroll
-    for (int w = 0; w < kTreeWaves; ++w) dn += dpart[w][i];
-    dn = dn * since + (r ? dsum[1][lr] + dsum[2 % NP][lr] : dsum[0][lr]);
-    const float inv = slot == kStateBad ? NAN : (m ? 1.f / dn : 0.f);
-    for (int ct = wave; ct < DT; ct += kTreeWaves) {
+      for (int w = 0; w < kSplit; ++w) dn += dpart[w][i];
+      dn = dn * since + (r ? dsum[1 % NP][lr] + dsum[2 % NP][lr] : dsum[0][lr]);
+      inv = slot == kStateBad ? NAN : (m ? 1.f / dn : 0.f);
+    }
+    if (fw < CG) {
+      const int ct = CG * g + fw;
       floatx16 o;
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         float x = 0.f;
 #pragma unroll
-        for (int w = 0; w < kTreeWaves; ++w) x += part[((w * DT + ct) * 16 + e) * 64 + lane];
+        for (int w = 0; w < kSplit; ++w) x += part[((w * RT * CG + r * CG + fw) * 16 + e) * 64 + lane];
         o[e] = m ? x * since : 0.f;  // (no NaN of the state where nothing is seen)
       }
 #pragma unroll
-      for (int jt = 0; jt <= r; ++jt)
+      for (int jt = 0; jt < RT; ++jt)
+        if (jt <= r) {
 #pragma unroll
-        for (int k2 = 0; k2 < 2; ++k2) {
-          uint4 vf[NT], pf[NPP];
-          read_terms<NT>(vl + ((jt * DT + ct) * 2 + k2) * NT * 64, vf);
-          read_terms<NPP>(&pl[r + jt][k2][0][0], pf);
-          o = mfma_terms<NT, NPP>(vf, pf, o);
+          for (int k2 = 0; k2 < 2; ++k2) {
+            uint4 vf[NT], pf[NPP];
+            read_terms<NT>(vl + ((jt * DT + ct) * 2 + k2) * NT * 64, vf);
+            read_terms<NPP>(&pl[r + jt][k2][0][0], pf);
+            o = mfma_terms<NT, NPP>(vf, pf, o);
+          }
         }
       if (odd) {
         // values that are not finite went in as zeros: NaN for the nodes that see them
@@ -242,12 +294,13 @@ __global__ __launch_bounds__(64 * kTreeWaves) void k_decay_tree(PoolArgs a) {
               if (((m >> j) & 1) && !finite(v.one(v.at(v.at(j), c)))) o[e] = NAN;
         }
       }
-      if (i < T)
+      if (i < T) {
 #pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const float o4[4] = {o[4 * g] * inv, o[4 * g + 1] * inv, o[4 * g + 2] * inv, o[4 * g + 3] * inv};
-          store4(z + static_cast<size_t>(i) * d, 32 * ct + 8 * g + 4 * lh, d, o4);
+        for (int e4 = 0; e4 < 4; ++e4) {
+          const float o4[4] = {o[4 * e4] * inv, o[4 * e4 + 1] * inv, o[4 * e4 + 2] * inv, o[4 * e4 + 3] * inv};
+          store4(z + static_cast<size_t>(i) * d, 32 * ct + 8 * e4 + 4 * lh, d, o4);
         }
+      }
     }
   }
 }
@@ -256,11 +309,11 @@ namespace {
 template <typename TX, int DK, bool ELU>
 hipError_t go(const PoolArgs& a, hipStream_t st) {
   constexpr int NT = sizeof(TX) == 2 ? 1 : 3, NP = sizeof(TX) == 2 ? 2 : 3;
-  const dim3 grid(static_cast<unsigned>(a.B) * a.H), block(64 * kTreeWaves);
+  const dim3 grid(static_cast<unsigned>(a.B) * a.H);
   if (a.T <= 32)
-    hipLaunchKernelGGL((k_decay_tree<TX, DK, NT, NP, 1, ELU>), grid, block, 0, st, a);
+    hipLaunchKernelGGL((k_decay_tree<TX, DK, NT, NP, 1, ELU>), grid, dim3(64 * kSplit), 0, st, a);
   else
-    hipLaunchKernelGGL((k_decay_tree<TX, DK, NT, NP, 2, ELU>), grid, block, 0, st, a);
+    hipLaunchKernelGGL((k_decay_tree<TX, DK, NT, NP, 2, ELU>), grid, dim3(128 * kSplit), 0, st, a);
   return hipGetLastError();
 }
 template <typename TX, bool ELU>

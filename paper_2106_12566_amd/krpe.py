@@ -366,50 +366,58 @@ def _decay_flags(nprf: bool, features: str) -> int:
 
 def _enqueue(name: str, device: torch.device, *args) -> None:
     """The C call `name` on the current stream of `device`, with that device the current one."""
-    fn = getattr(load(), name)
-    if torch.cuda.current_device() == device.index:
-        _check(fn(*args, _stream(device)), name)
+    index = device.index
+    fn = getattr(_lib or load(), name)
+    if torch.cuda.current_device() == index:
+        st = fn(*args, torch._C._cuda_getCurrentRawStream(index))
     else:
         with torch.cuda.device(device):
-            _check(fn(*args, _stream(device)), name)
+            st = fn(*args, torch._C._cuda_getCurrentRawStream(index))
+    if st != 0:
+        _check(st, name)
 
 
-def _decay_inputs(tensors: dict, rate: torch.Tensor, W: torch.Tensor | None, features: str, dims: int):
-    """Checked, contiguous inputs of one shape [B, H, (rows,) d] and type; rate, W and m."""
+def _decay_inputs(names: tuple, tensors: tuple, rate: torch.Tensor, W: torch.Tensor | None, features: str, dims: int):
+    """Checked, contiguous inputs of one shape [B, H, (rows,) d] and type; rate, W, m and that shape.
+
+    (A token's call is a few microseconds: every attribute is read once.)"""
     out = []
-    first = None
-    for name, t in tensors.items():
+    shape = dtype = device = None
+    for name, t in zip(names, tensors):
         t = _gpu(t, name)
-        if first is None:
-            first = t
-            if t.dim() != dims:
+        if shape is None:
+            shape, dtype, device = t.shape, t.dtype, t.device
+            if len(shape) != dims:
                 raise KrpeError(f"{name} must have {dims} dimensions")
-        elif t.shape != first.shape or t.dtype != first.dtype:
-            raise KrpeError(f"{', '.join(tensors)} must share shape and dtype")
+            if dtype not in DTYPES:
+                raise KrpeError(f"{name} must be float32 or bfloat16, got {dtype}")
+        elif t.shape != shape or t.dtype != dtype:
+            raise KrpeError(f"{', '.join(names)} must share shape and dtype")
+        elif t.device != device:
+            _elsewhere(t, device)
         out.append(t)
-    _dtype_code(first, next(iter(tensors)))
-    H, d = first.shape[1], first.shape[-1]
+    H, d = shape[1], shape[-1]
     rate = _gpu(rate, "rate")
     if rate.shape != (H,) or rate.dtype != torch.float32:
         raise KrpeError("rate must be float32 [H]")
     W, m = _proj(W, H, d, features)
-    _one_device(first.device, *out[1:], rate, W)
-    return out, rate, W, m
+    if rate.device != device or (W is not None and W.device != device):
+        _elsewhere(rate if rate.device != device else W, device)
+    return out, rate, W, m, shape, device
 
 
-def _one_device(device: torch.device, *tensors) -> None:
-    for t in tensors:
-        if t is not None and t.device != device:
-            raise KrpeError(f"all tensors must be on one GPU: {t.device} and {device}")
+def _elsewhere(t: torch.Tensor, device: torch.device) -> None:
+    raise KrpeError(f"all tensors must be on one GPU: {t.device} and {device}")
 
 
 def _ints(t: torch.Tensor | None, name: str, shape: tuple, device: torch.device) -> torch.Tensor | None:
     if t is None:
         return None
     t = _gpu(t, name)
-    if t.dtype != torch.int32 or tuple(t.shape) != shape:
+    if t.dtype != torch.int32 or t.shape != shape:
         raise KrpeError(f"{name} must be int32 {list(shape)}")
-    _one_device(device, t)
+    if t.device != device:
+        _elsewhere(t, device)
     return t
 
 
@@ -417,12 +425,18 @@ def _pool(state: torch.Tensor, H: int, d: int, m: int, device: torch.device) -> 
     """The number of slots of a pool, which has to be contiguous (it is changed in place)."""
     if not isinstance(state, torch.Tensor) or not state.is_cuda:
         raise KrpeError("state must be on a GPU (libkrpe has no CPU path)")
-    if state.dim() != 4 or state.shape[1:] != (H, d + 1, m) or state.dtype != torch.float32:
+    shape = state.shape
+    if len(shape) != 4 or shape != (shape[0], H, d + 1, m) or state.dtype != torch.float32:
         raise KrpeError(f"state must be float32 [slots, {H}, {d + 1}, {m}]")
     if not state.is_contiguous():
         raise KrpeError("state must be contiguous")
-    _one_device(device, state)
-    return state.shape[0]
+    if state.device != device:
+        _elsewhere(state, device)
+    return shape[0]
+
+
+def _at(t: torch.Tensor | None) -> int | None:
+    return None if t is None else t.data_ptr()
 
 
 def _like(out: torch.Tensor | None, x: torch.Tensor, zeros: bool) -> torch.Tensor:
@@ -431,7 +445,8 @@ def _like(out: torch.Tensor | None, x: torch.Tensor, zeros: bool) -> torch.Tenso
         return torch.zeros_like(x) if zeros else torch.empty_like(x)
     if not isinstance(out, torch.Tensor) or out.shape != x.shape or out.dtype != x.dtype or not out.is_contiguous():
         raise KrpeError("out must be a contiguous tensor of q's shape and dtype")
-    _one_device(x.device, out)
+    if out.device != x.device:
+        _elsewhere(out, x.device)
     return out
 
 
@@ -440,7 +455,8 @@ def _space(workspace: torch.Tensor | None, need: int, device: torch.device) -> t
         return torch.empty(max(need, 1), dtype=torch.uint8, device=device)
     if workspace.dtype != torch.uint8 or workspace.numel() < need or not workspace.is_contiguous():
         raise KrpeError(f"workspace must hold at least {need} bytes (uint8)")
-    _one_device(device, workspace)
+    if workspace.device != device:
+        _elsewhere(workspace, device)
     return workspace
 
 
@@ -465,9 +481,8 @@ def decay_attention_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, rate:
     ``lens``: int32 [B], the positions of each sequence; rows of q, k, v behind them are
     not read and rows of ``out`` stay as they were (zeros without ``out``)."""
     flags = _decay_flags(nprf, features)
-    (q, k, v), rate, W, m = _decay_inputs({"q": q, "k": k, "v": v}, rate, W, features, 4)
-    B, H, n, d = q.shape
-    dev = q.device
+    (q, k, v), rate, W, m, shape, dev = _decay_inputs(("q", "k", "v"), (q, k, v), rate, W, features, 4)
+    B, H, n, d = shape
     nslots = 0
     if state is not None:
         nslots = _pool(state, H, d, m, dev)
@@ -477,8 +492,8 @@ def decay_attention_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, rate:
     slots, lens = _ints(slots, "slots", (B,), dev), _ints(lens, "lens", (B,), dev)
     z = _like(out, q, lens is not None)
     ws = _space(workspace, int(load().krpe_decay_fwd_workspace(B, H, n, d, m, flags)), dev)
-    _enqueue("krpe_decay_fwd", dev, _ptr(q), _ptr(k), _ptr(v), DTYPES[q.dtype], _ptr(rate), _ptr(W), _ptr(z),
-             _ptr(state), _ptr(slots), nslots, _ptr(lens), B, H, n, d, m, flags, ws.data_ptr(), ws.numel())
+    _enqueue("krpe_decay_fwd", dev, _at(q), _at(k), _at(v), DTYPES[q.dtype], _at(rate), _at(W), _at(z),
+             _at(state), _at(slots), nslots, _at(lens), B, H, n, d, m, flags, ws.data_ptr(), ws.numel())
     return z
 
 
@@ -492,13 +507,13 @@ def decay_attention_bwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, rate:
     """Gradients (dq, dk, dv) [B,H,n,d] in q's type of sum(dz * z), z = decay_attention_fwd(q, k, v, rate, W)
     from empty states, rate and W fixed.  Rows behind ``lens`` are zero."""
     flags = _decay_flags(nprf, features)
-    (q, k, v, dz), rate, W, m = _decay_inputs({"q": q, "k": k, "v": v, "dz": dz}, rate, W, features, 4)
-    B, H, n, d = q.shape
-    lens = _ints(lens, "lens", (B,), q.device)
+    (q, k, v, dz), rate, W, m, shape, dev = _decay_inputs(("q", "k", "v", "dz"), (q, k, v, dz), rate, W, features, 4)
+    B, H, n, d = shape
+    lens = _ints(lens, "lens", (B,), dev)
     dq, dk, dv = (_like(None, q, lens is not None) for _ in range(3))
-    ws = _space(workspace, int(load().krpe_decay_bwd_workspace(B, H, n, d, m, flags)), q.device)
-    _enqueue("krpe_decay_bwd", q.device, _ptr(q), _ptr(k), _ptr(v), DTYPES[q.dtype], _ptr(rate), _ptr(W), _ptr(dz),
-             _ptr(dq), _ptr(dk), _ptr(dv), _ptr(lens), B, H, n, d, m, flags, ws.data_ptr(), ws.numel())
+    ws = _space(workspace, int(load().krpe_decay_bwd_workspace(B, H, n, d, m, flags)), dev)
+    _enqueue("krpe_decay_bwd", dev, _at(q), _at(k), _at(v), DTYPES[q.dtype], _at(rate), _at(W), _at(dz),
+             _at(dq), _at(dk), _at(dv), _at(lens), B, H, n, d, m, flags, ws.data_ptr(), ws.numel())
     return dq, dk, dv
 
 
@@ -508,13 +523,13 @@ def decay_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, rate
     """One token of every sequence: its k, v [B,H,d] go into the states, z [B,H,d] is its output.
     Allocates nothing with ``out`` (a captured graph may replay it)."""
     flags = _decay_flags(nprf, features)
-    (q, k, v), rate, W, m = _decay_inputs({"q": q, "k": k, "v": v}, rate, W, features, 3)
-    B, H, d = q.shape
-    nslots = _pool(state, H, d, m, q.device)
-    slots = _ints(slots, "slots", (B,), q.device)
+    (q, k, v), rate, W, m, shape, dev = _decay_inputs(("q", "k", "v"), (q, k, v), rate, W, features, 3)
+    B, H, d = shape
+    nslots = _pool(state, H, d, m, dev)
+    slots = _ints(slots, "slots", (B,), dev)
     z = _like(out, q, False)
-    _enqueue("krpe_decay_step", q.device, _ptr(q), _ptr(k), _ptr(v), DTYPES[q.dtype], _ptr(rate), _ptr(W), _ptr(z),
-             _ptr(state), _ptr(slots), nslots, B, H, d, m, flags)
+    _enqueue("krpe_decay_step", dev, _at(q), _at(k), _at(v), DTYPES[q.dtype], _at(rate), _at(W), _at(z),
+             _at(state), _at(slots), nslots, B, H, d, m, flags)
     return z
 
 
@@ -526,15 +541,15 @@ def decay_attention_tree(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, pare
     of the sequence's last token; a node with any other parent, and what is below it, gets zeros.
     The states stay as they are: decay_attention_commit takes the accepted nodes in."""
     flags = _decay_flags(nprf, features)
-    (q, k, v), rate, W, m = _decay_inputs({"q": q, "k": k, "v": v}, rate, W, features, 4)
-    B, H, T, d = q.shape
-    nslots = _pool(state, H, d, m, q.device)
+    (q, k, v), rate, W, m, shape, dev = _decay_inputs(("q", "k", "v"), (q, k, v), rate, W, features, 4)
+    B, H, T, d = shape
+    nslots = _pool(state, H, d, m, dev)
     if parent is None:
         raise KrpeError("parent must be int32 [B, T]")
-    parent, slots = _ints(parent, "parent", (B, T), q.device), _ints(slots, "slots", (B,), q.device)
+    parent, slots = _ints(parent, "parent", (B, T), dev), _ints(slots, "slots", (B,), dev)
     z = _like(out, q, False)
-    _enqueue("krpe_decay_tree", q.device, _ptr(q), _ptr(k), _ptr(v), DTYPES[q.dtype], _ptr(parent), _ptr(rate), _ptr(W),
-             _ptr(z), _ptr(state), _ptr(slots), nslots, B, H, T, d, m, flags)
+    _enqueue("krpe_decay_tree", dev, _at(q), _at(k), _at(v), DTYPES[q.dtype], _at(parent), _at(rate), _at(W),
+             _at(z), _at(state), _at(slots), nslots, B, H, T, d, m, flags)
     return z
 
 
@@ -544,15 +559,15 @@ def decay_attention_commit(k: torch.Tensor, v: torch.Tensor, path: torch.Tensor,
     """Takes tokens path[b, 0], path[b, 1], .. of k, v [B,H,T,d] into the states, up to the first entry
     outside [0, T).  ``path``: int32 [B,P]."""
     flags = _decay_flags(nprf, features)
-    (k, v), rate, W, m = _decay_inputs({"k": k, "v": v}, rate, W, features, 4)
-    B, H, T, d = k.shape
-    nslots = _pool(state, H, d, m, k.device)
+    (k, v), rate, W, m, shape, dev = _decay_inputs(("k", "v"), (k, v), rate, W, features, 4)
+    B, H, T, d = shape
+    nslots = _pool(state, H, d, m, dev)
     if not isinstance(path, torch.Tensor) or path.dim() != 2:
         raise KrpeError("path must be int32 [B, P]")
-    path = _ints(path, "path", (B, path.shape[1]), k.device)
-    slots = _ints(slots, "slots", (B,), k.device)
-    _enqueue("krpe_decay_commit", k.device, _ptr(k), _ptr(v), DTYPES[k.dtype], _ptr(path), _ptr(rate), _ptr(W),
-             _ptr(state), _ptr(slots), nslots, B, H, T, path.shape[1], d, m, flags)
+    path = _ints(path, "path", (B, path.shape[1]), dev)
+    slots = _ints(slots, "slots", (B,), dev)
+    _enqueue("krpe_decay_commit", dev, _at(k), _at(v), DTYPES[k.dtype], _at(path), _at(rate), _at(W),
+             _at(state), _at(slots), nslots, B, H, T, path.shape[1], d, m, flags)
 
 
 def decay_state_copy(state: torch.Tensor, src: torch.Tensor, dst: torch.Tensor) -> None:
@@ -568,5 +583,5 @@ def decay_state_copy(state: torch.Tensor, src: torch.Tensor, dst: torch.Tensor) 
     src, dst = _ints(src, "src", (src.shape[0],), state.device), _ints(dst, "dst", (src.shape[0],), state.device)
     if dst is None:
         raise KrpeError("dst must be int32 [count]")
-    _enqueue("krpe_decay_state_copy", state.device, _ptr(state), _ptr(src), _ptr(dst), src.shape[0], nslots, H, rows - 1,
+    _enqueue("krpe_decay_state_copy", state.device, _at(state), _at(src), _at(dst), src.shape[0], nslots, H, rows - 1,
              m)
