@@ -34,17 +34,23 @@ namespace krpe {
 constexpr int kChunk = 128;  // positions of a chunk: four row tiles of 32
 constexpr int kStateNone = -1, kStateBad = -2;
 
-// The pool's row of sequence b: kStateNone for a negative slot of -1 (no state:
-// zeros before, not kept), kStateBad for one outside the pool or named by another
-// sequence of the call too (two would write one state).  Every lane gets it.
-__device__ __forceinline__ int slot_of(const int* __restrict__ slots, int b, int B, int nslots) {
+// The pool's row of sequence b: kStateNone for a negative slot of -1 (no state: zeros before, not
+// kept), kStateBad for one outside the pool or named by another sequence of the call too (two
+// would write one state).  Every lane gets it.  slot_in() leaves the last to check_slot(), so that
+// a state can be asked for, not written, before the other sequences' slots are there.
+__device__ __forceinline__ int slot_in(const int* __restrict__ slots, int b, int nslots) {
   if (!slots) return b;
   const int s = slots[b];
-  if (s == -1) return kStateNone;
-  if (s < 0 || s >= nslots) return kStateBad;
+  return s == -1 ? kStateNone : (s < 0 || s >= nslots ? kStateBad : s);
+}
+__device__ __forceinline__ int check_slot(const int* __restrict__ slots, int slot, int b, int B) {
+  if (!slots || slot < 0) return slot;
   int twice = 0;
-  for (int j = threadIdx.x & 63; j < B; j += 64) twice |= j != b && slots[j] == s;
-  return __any(twice) ? kStateBad : s;
+  for (int j = threadIdx.x & 63; j < B; j += 64) twice |= j != b && slots[j] == slot;
+  return __any(twice) ? kStateBad : slot;
+}
+__device__ __forceinline__ int slot_of(const int* __restrict__ slots, int b, int B, int nslots) {
+  return check_slot(slots, slot_in(slots, b, nslots), b, B);
 }
 
 // (a rate of inf weighs 1 at distance 0 and 0 beyond)

@@ -33,7 +33,7 @@ __device__ __forceinline__ int path_rows(const int* __restrict__ path, int P, in
 template <typename TX, typename TV, int DK, int NP, int NV, bool ELU, Sums MODE, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, DK <= 4 ? 2 : 1) void k_decay_states(DecayArgs a) {
   constexpr bool BACK = MODE == Sums::kBack, PATH = MODE == Sums::kPath, WHOLE = sizeof(TX) == 4;
-  constexpr int NSX = kTermsX<TX>, DT = DK / 2, PB = WHOLE || DK == 8 ? 2 : 4;
+  constexpr int NSX = kTermsX<TX>, DT = DK / 2, PB = WHOLE || DK == 8 || PATH ? 2 : 4;
   constexpr int BPW = (PB + WAVES - 1) / WAVES;  // blocks of x that a wave stages
   __shared__ __align__(16) uint4 xl[PB * DK * NSX * kFragLanes], vl[PB * DT * 2 * NV * kFragLanes];
   __shared__ __align__(16) float fr[32 * PB], fc[32 * PB], ff[32 * PB], fd[BACK ? 32 * PB : 4];
@@ -44,7 +44,7 @@ __global__ __launch_bounds__(64 * WAVES, DK <= 4 ? 2 : 1) void k_decay_states(De
   const int* __restrict__ path = PATH ? a.path + static_cast<size_t>(b) * a.P : nullptr;
   const int rows = PATH ? path_rows(path, a.P, a.n) : rows_of(a.lens, b, a.n);
   const bool whole = PATH || a.nseg == 1;  // uniform
-  const int slot = !BACK && whole && a.state ? slot_of(a.slots, b, a.B, a.nslots) : kStateNone;
+  int slot = !BACK && whole && a.state ? slot_in(a.slots, b, a.nslots) : kStateNone;
   if (PATH && (slot < 0 || rows == 0)) return;
   const int c0 = PATH ? 0 : seg * a.segc, c1 = PATH ? (rows + kChunk - 1) / kChunk
                                                     : min(min(a.nchunk, c0 + a.segc), (rows + kChunk - 1) / kChunk);
@@ -102,6 +102,8 @@ __global__ __launch_bounds__(64 * WAVES, DK <= 4 ? 2 : 1) void k_decay_states(De
       }
     if (lh == 0) sum = st[static_cast<size_t>(d) * M + l];
   }
+  slot = check_slot(a.slots, slot, b, a.B);
+  if (PATH && slot < 0) return;
   auto store = [&](float* __restrict__ to, int width) {
     const float s = sum + __shfl_xor(sum, 32);
     if (l >= width) return;
@@ -216,7 +218,7 @@ __global__ __launch_bounds__(64 * WAVES, DK <= 4 ? 2 : 1) void k_decay_states(De
   }
   if (!whole)
     store((BACK ? a.totb : a.tot) + (static_cast<size_t>(bh) * a.nseg + seg) * cells, Mp);
-  else if (st)
+  else if (slot >= 0)
     store(st, M);
 }
 

@@ -8,131 +8,142 @@
 
 namespace krpe {
 
-// Features of R rows x [R][d] in LDS (fp32), f [R][M4] (zeros from M to M4).  A group of 2^g
-// lanes takes a feature, each a part of its dimensions.
-template <int R, bool ELU>
-__device__ __forceinline__ void row_features(const float* __restrict__ x, const float* __restrict__ sq,
-                                             const float* __restrict__ W, int d, int M, int M4, float log_m, bool nprf,
-                                             float* __restrict__ f) {
-  for (int l = threadIdx.x; l < M4; l += blockDim.x) {
-    float acc[R];
-#pragma unroll
-    for (int r = 0; r < R; ++r) acc[r] = 0.f;
-    if (l < M) {
-      if constexpr (ELU) {
-#pragma unroll
-        for (int r = 0; r < R; ++r) acc[r] = x[r * d + l];
-      } else {
-        const float* __restrict__ w = W + static_cast<size_t>(l) * d;
-        if (d % 4 == 0) {
-          for (int c = 0; c < d; c += 4) {
-            const float4 u = *reinterpret_cast<const float4*>(w + c);
-#pragma unroll
-            for (int r = 0; r < R; ++r) {
-              const float4 y = *reinterpret_cast<const float4*>(x + r * d + c);
-              acc[r] = fmaf(u.x, y.x, acc[r]), acc[r] = fmaf(u.y, y.y, acc[r]);
-              acc[r] = fmaf(u.z, y.z, acc[r]), acc[r] = fmaf(u.w, y.w, acc[r]);
-            }
-          }
-        } else {
-          for (int c = 0; c < d; ++c)
-#pragma unroll
-            for (int r = 0; r < R; ++r) acc[r] = fmaf(w[c], x[r * d + c], acc[r]);
-        }
-      }
-    }
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-      float o = 0.f;
-      if (l < M) {
-        const float s = nprf ? (sq[r] > 0.f ? rsqrtf(sq[r]) : 0.f) : 1.f;
-        if constexpr (ELU) {
-          const float y = acc[r] * s;
-          o = y > 0.f ? y + 1.f : expf(y);
-        } else {
-          const float half = nprf ? (sq[r] > 0.f ? 0.5f : 0.f) : 0.5f * sq[r];
-          o = expf(acc[r] * s - half + log_m);
-        }
-      }
-      f[r * M4 + l] = o;
-    }
-  }
-}
-
-// The sums of squares of R rows in LDS, one wave a row.
-template <int R>
-__device__ __forceinline__ void row_squares(const float* __restrict__ x, int d, float* __restrict__ sq) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
-  for (int r = wave; r < R; r += waves) {
-    float s = 0.f;
-    for (int c = lane; c < d; c += 64) s = fmaf(x[r * d + c], x[r * d + c], s);
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) s += __shfl_xor(s, o);
-    if (lane == 0) sq[r] = s;
-  }
-}
-
-// Lanes of a wave on one row of a state (a power of two), four features each.
-__device__ __forceinline__ int lanes_of(int M4) {
-  int n = 1;
-  while (n < 64 && n * 4 < M4) n <<= 1;
-  return n;
-}
-__device__ __forceinline__ float4 load_cells(const float* __restrict__ p, int l, int M, bool vec) {
-  if (vec) return *reinterpret_cast<const float4*>(p + l);
-  return make_float4(p[l], l + 1 < M ? p[l + 1] : 0.f, l + 2 < M ? p[l + 2] : 0.f, l + 3 < M ? p[l + 3] : 0.f);
-}
-__device__ __forceinline__ void store_cells(float* __restrict__ p, int l, int M, bool vec, float4 v) {
+typedef unsigned uintx4 __attribute__((ext_vector_type(4)));
+// Four cells of a state's row c from feature l through its buffer: what lies past the last row or the
+// row's end (M) reads as zero and is not written.
+__device__ __forceinline__ float4 load_cells(const Rows<float>& st, int c, int l, bool vec) {
+  const uint32_t o = l < st.d ? st.at(c) + 4u * l : kOut;
   if (vec) {
-    *reinterpret_cast<float4*>(p + l) = v;
+    const uint4 u = st.b128(o);
+    return make_float4(__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w));
+  }
+  return make_float4(st.one(o), st.one(l + 1 < st.d ? o + 4 : kOut), st.one(l + 2 < st.d ? o + 8 : kOut),
+                     st.one(l + 3 < st.d ? o + 12 : kOut));
+}
+__device__ __forceinline__ void store_cells(const Rows<float>& st, int c, int l, bool vec, float4 v) {
+  const uint32_t o = l < st.d ? st.at(c) + 4u * l : kOut;
+  const uintx4 u = {__float_as_uint(v.x), __float_as_uint(v.y), __float_as_uint(v.z), __float_as_uint(v.w)};
+  if (vec) {
+    __builtin_amdgcn_raw_buffer_store_b128(u, st.r, o, 0, 0);
   } else {
-    p[l] = v.x;
-    if (l + 1 < M) p[l + 1] = v.y;
-    if (l + 2 < M) p[l + 2] = v.z;
-    if (l + 3 < M) p[l + 3] = v.w;
+#pragma unroll
+    for (int t = 0; t < 4; ++t) __builtin_amdgcn_raw_buffer_store_b32(u[t], st.r, l + t < st.d ? o + 4 * t : kOut, 0, 0);
   }
 }
 
 // One token of a sequence and head: A <- e^-rate A + [v; 1] phi(k)^T, z = A phi(q).
-template <typename TX, bool ELU>
-__global__ __launch_bounds__(256) void k_decay_step(PoolArgs a) {
+//
+// Bound by the state, which is read and written once.  L lanes have a row's features, four each
+// (256 of them at a time), and a thread K rows at a time: the first K are asked for before the
+// token's features are worked out.  K sums over L lanes take fewer than K + log2(L) exchanges,
+// halving at each the rows that a lane has a part of.
+// 256 x 16 heads, 256 features, d = 64 (545 MB): 119 us, 4.6 TB/s (d = 128: 5.0; a plain copy 5.1).
+// With the state read after the features and a row summed at a time 142 us; with 8 or 16 rows at a
+// time 129 and 186 us and with six waves a SIMD 149 us, as registers run short.
+template <typename TX, int L, bool ELU>
+__global__ __launch_bounds__(256, 4) void k_decay_step(PoolArgs a) {
+  constexpr int K = 4, R = 256 / L;  // rows of a thread at a time, rows side by side
   extern __shared__ __align__(16) float sm[];
   const int d = a.d, M = a.M, M4 = (M + 3) & ~3, d4 = (d + 3) & ~3;
-  float *x = sm, *f = sm + 2 * d4, *v = f + 2 * M4, *num = v + d + 1;  // num: d + 1 sums
-  __shared__ float sq[2];
+  float *xq = sm, *xk = xq + d4, *fq = xk + d4, *fk = fq + M4, *v = fk + M4, *num = v + d4 + 4;  // v, num: d + 1
   const int b = blockIdx.x / a.H, h = blockIdx.x % a.H;
-  const int slot = slot_of(a.slots, b, a.B, a.nslots);
-  const size_t row = static_cast<size_t>(blockIdx.x) * d;
-  for (int c = threadIdx.x; c < d; c += 256) {
-    x[c] = to_f32(static_cast<const TX*>(a.q)[row + c]);
-    x[d + c] = to_f32(static_cast<const TX*>(a.k)[row + c]);
-    v[c] = to_f32(static_cast<const TX*>(a.v)[row + c]);
-  }
-  if (threadIdx.x == 0) v[d] = 1.f;
-  __syncthreads();
-  row_squares<2>(x, d, sq);
-  __syncthreads();
-  row_features<2, ELU>(x, sq, a.W + static_cast<size_t>(h) * M * d, d, M, M4, a.log_m, a.nprf, f);
-  __syncthreads();
-  const int L = lanes_of(M4), lane = threadIdx.x % L, per = 256 / L;
-  const float w = decay(rate_log2(a.rate[h]), 1);
+  const int lane = threadIdx.x % L, r0 = threadIdx.x / L;
+  int slot = slot_in(a.slots, b, a.nslots);
   const bool vec = M % 4 == 0;
-  float* __restrict__ st = slot >= 0 ? a.state + (static_cast<size_t>(slot) * a.H + h) * (d + 1) * M : nullptr;
-  for (int c0 = 0; c0 <= d; c0 += per) {
-    const int c = c0 + threadIdx.x / L;
-    float s = 0.f;
-    if (c <= d)
-      for (int l = 4 * lane; l < M; l += 4 * L) {
-        const float4 fq = *reinterpret_cast<const float4*>(f + l), fk = *reinterpret_cast<const float4*>(f + M4 + l);
-        float4 u = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (st) u = load_cells(st + static_cast<size_t>(c) * M, l, M, vec);
-        u.x = fmaf(w, u.x, v[c] * fk.x), u.y = fmaf(w, u.y, v[c] * fk.y);
-        u.z = fmaf(w, u.z, v[c] * fk.z), u.w = fmaf(w, u.w, v[c] * fk.w);
-        if (st) store_cells(st + static_cast<size_t>(c) * M, l, M, vec, u);
-        s = fmaf(u.x, fq.x, s), s = fmaf(u.y, fq.y, s), s = fmaf(u.z, fq.z, s), s = fmaf(u.w, fq.w, s);
+  const Rows<float> st(slot >= 0 ? a.state + (static_cast<size_t>(slot) * a.H + h) * (d + 1) * M : a.state,
+                       slot >= 0 ? d + 1 : 0, M);
+  const size_t row = static_cast<size_t>(blockIdx.x) * d;
+  float4 u[K];
+  auto fetch = [&](int l, int p) {
+#pragma unroll
+    for (int i = 0; i < K; ++i) u[i] = load_cells(st, (p * K + i) * R + r0, l, vec);
+  };
+  float sq = 0.f, sk = 0.f;  // squares of the rows, over each wave by itself
+  for (int c = threadIdx.x & 63; c < d; c += 64) {
+    const float y = to_f32(static_cast<const TX*>(a.q)[row + c]), x = to_f32(static_cast<const TX*>(a.k)[row + c]);
+    const float w = to_f32(static_cast<const TX*>(a.v)[row + c]);
+    sq = fmaf(y, y, sq), sk = fmaf(x, x, sk);
+    if (threadIdx.x < 64) xq[c] = y, xk[c] = x, v[c] = w, num[c] = 0.f;
+  }
+  if (threadIdx.x == 0) v[d] = 1.f, num[d] = 0.f;
+  fetch(4 * lane, 0);
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) sq += __shfl_xor(sq, o), sk += __shfl_xor(sk, o);
+  __syncthreads();
+  for (int l = threadIdx.x; l < M4; l += 256) {
+    float p = 0.f, q = 0.f;
+    if (l < M) {
+      if constexpr (ELU) {
+        p = xk[l], q = xq[l];
+      } else {
+        const float* __restrict__ w = a.W + (static_cast<size_t>(h) * M + l) * d;
+        if (d % 4 == 0) {
+#pragma unroll 4
+          for (int c = 0; c < d; c += 4) {
+            const float4 g = *reinterpret_cast<const float4*>(w + c);
+            const float4 x = *reinterpret_cast<const float4*>(xk + c), y = *reinterpret_cast<const float4*>(xq + c);
+            p = fmaf(g.x, x.x, p), p = fmaf(g.y, x.y, p), p = fmaf(g.z, x.z, p), p = fmaf(g.w, x.w, p);
+            q = fmaf(g.x, y.x, q), q = fmaf(g.y, y.y, q), q = fmaf(g.z, y.z, q), q = fmaf(g.w, y.w, q);
+          }
+        } else {
+          for (int c = 0; c < d; ++c) p = fmaf(w[c], xk[c], p), q = fmaf(w[c], xq[c], q);
+        }
       }
-    for (int o = 1; o < L; o <<= 1) s += __shfl_xor(s, o);
-    if (c <= d && lane == 0) num[c] = s;
+    }
+    auto phi = [&](float s, float square) {
+      const bool nz = square > 0.f;
+      if (a.nprf) s *= nz ? rsqrtf(square) : 0.f;
+      if constexpr (ELU) return s > 0.f ? s + 1.f : expf(s);
+      return expf(s - (a.nprf ? (nz ? 0.5f : 0.f) : 0.5f * square) + a.log_m);
+    };
+    fk[l] = l < M ? phi(p, sk) : 0.f;
+    fq[l] = l < M ? phi(q, sq) : 0.f;
+  }
+  slot = check_slot(a.slots, slot, b, a.B);
+  const float w = decay(rate_log2(a.rate[h]), 1);
+  __syncthreads();
+  for (int l = 4 * lane; l < M4 || l < 4 * L; l += 4 * L) {  // (all lanes go round together)
+    float4 gq = make_float4(0.f, 0.f, 0.f, 0.f), gk = gq;
+    if (l < M) gq = *reinterpret_cast<const float4*>(fq + l), gk = *reinterpret_cast<const float4*>(fk + l);
+    for (int p = 0; p * K * R <= d; ++p) {
+      if (p || l >= 4 * L) fetch(l, p);
+      float s[K];
+#pragma unroll
+      for (int i = 0; i < K; ++i) {
+        const int c = (p * K + i) * R + r0;
+        const float y = c <= d ? v[c] : 0.f;
+        u[i].x = fmaf(w, u[i].x, y * gk.x), u[i].y = fmaf(w, u[i].y, y * gk.y);
+        u[i].z = fmaf(w, u[i].z, y * gk.z), u[i].w = fmaf(w, u[i].w, y * gk.w);
+        if (slot >= 0) store_cells(st, c, l, vec, u[i]);
+        s[i] = fmaf(u[i].x, gq.x, fmaf(u[i].y, gq.y, fmaf(u[i].z, gq.z, u[i].w * gq.w)));
+      }
+      // lane bit by lane bit, the half of the rows that stays takes the other lane's parts
+      int n = K, mine = 0;
+#pragma unroll
+      for (int o = L / 2; o >= 1; o >>= 1) {
+        if (n > 1) {
+          n >>= 1;
+          const bool up = lane & o;
+#pragma unroll
+          for (int i = 0; i < K / 2; ++i)
+            if (i < n) {
+              const float keep = up ? s[i + n] : s[i], send = up ? s[i] : s[i + n];
+              s[i] = keep + __shfl_xor(send, o);
+            }
+          mine += up ? n : 0;
+        } else {
+          s[0] += __shfl_xor(s[0], o);
+        }
+      }
+      constexpr int spare = L > K ? L / K - 1 : 0;  // lanes that ended with the same row
+      if (!(lane & spare))
+#pragma unroll
+        for (int i = 0; i < K; ++i)
+          if (i < n) {
+            const int c = (p * K + mine + i) * R + r0;
+            if (c <= d) num[c] += s[i];
+          }
+    }
   }
   __syncthreads();
   TX* __restrict__ z = static_cast<TX*>(a.z) + row;
@@ -178,14 +189,28 @@ __global__ __launch_bounds__(64) __attribute__((amdgpu_waves_per_eu(1))) void k_
   }
 }
 
-hipError_t launch_decay_step(bool bf16, bool elu, const PoolArgs& a, hipStream_t st) {
+namespace {
+template <typename TX, bool ELU>
+void step(const PoolArgs& a, hipStream_t st) {
   const int M4 = (a.M + 3) & ~3, d4 = (a.d + 3) & ~3;
   const dim3 grid(static_cast<unsigned>(a.B) * a.H), block(256);
-  const size_t lds = (2 * d4 + 2 * M4 + 2 * (a.d + 1)) * sizeof(float);
-  if (bf16)
-    elu ? k_decay_step<uint16_t, true><<<grid, block, lds, st>>>(a) : k_decay_step<uint16_t, false><<<grid, block, lds, st>>>(a);
+  const size_t lds = (4 * d4 + 2 * M4 + 8) * sizeof(float);
+  if (M4 <= 32)
+    hipLaunchKernelGGL((k_decay_step<TX, 8, ELU>), grid, block, lds, st, a);
+  else if (M4 <= 64)
+    hipLaunchKernelGGL((k_decay_step<TX, 16, ELU>), grid, block, lds, st, a);
+  else if (M4 <= 128)
+    hipLaunchKernelGGL((k_decay_step<TX, 32, ELU>), grid, block, lds, st, a);
   else
-    elu ? k_decay_step<float, true><<<grid, block, lds, st>>>(a) : k_decay_step<float, false><<<grid, block, lds, st>>>(a);
+    hipLaunchKernelGGL((k_decay_step<TX, 64, ELU>), grid, block, lds, st, a);
+}
+}  // namespace
+
+hipError_t launch_decay_step(bool bf16, bool elu, const PoolArgs& a, hipStream_t st) {
+  if (bf16)
+    elu ? step<uint16_t, true>(a, st) : step<uint16_t, false>(a, st);
+  else
+    elu ? step<float, true>(a, st) : step<float, false>(a, st);
   return hipGetLastError();
 }
 

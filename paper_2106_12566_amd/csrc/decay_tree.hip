@@ -56,7 +56,7 @@ __global__ __launch_bounds__(64 * kSplit * RT, sizeof(TX) == 2 && DK <= 4 ? 2 : 
 #pragma unroll
     for (int ks = 0; ks < DK; ++ks) load_weights<ELU>(W, f0 + lr, 16 * ks + 8 * lh, w8[ks]);
   };
-  const int slot = slot_of(a.slots, b, a.B, a.nslots);
+  int slot = slot_in(a.slots, b, a.nslots);
   const float* __restrict__ st = slot >= 0 ? a.state + (static_cast<size_t>(slot) * a.H + h) * (d + 1) * M : nullptr;
   const Rows<float> sr(st ? st : a.state, st ? d + 1 : 0, M);  // (no state: zeros)
   const bool vec = M % 4 == 0;
@@ -245,6 +245,7 @@ __global__ __launch_bounds__(64 * kSplit * RT, sizeof(TX) == 2 && DK <= 4 ? 2 : 
       for (int n = 0; n < NPP; ++n) pl[t][k2][n][lane] = f[n];
     }
   }
+  slot = check_slot(a.slots, slot, b, a.B);
   TX* __restrict__ z = static_cast<TX*>(a.z) + base;
   const int i = 32 * r + lr;
   const unsigned long long m = seen[i];
