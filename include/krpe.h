@@ -333,7 +333,8 @@ krpe_status_t krpe_attention_fwd_stats(const void* ws, size_t ws_bytes, int B, i
  *   b has slot b, nslots >= B) names each sequence's; -1: none, zeros before the call and not
  *   kept after it.  A slot outside [-1, nslots), or one that two sequences of a call name, is
  *   refused on the device: these sequences' z is NaN and the pool stays as it was.
- * - features have to stay within fp32's range, as krpe_feature_map's.  A q, k or v element that
+ * - features have to stay within fp32's range, as krpe_feature_map's (with fp32 q, k, v: |W| < 65504
+ *   too).  A q, k or v element that
  *   is not finite makes what sees it not finite, and nothing else (gradients: its whole sequence
  *   and head).
  * - rate and integer arrays need 4-byte alignment, all others 16 bytes.

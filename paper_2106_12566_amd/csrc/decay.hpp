@@ -16,8 +16,10 @@
 // two takes the six of at least 2^-16 of it.  Where the result is rounded to
 // bf16 (1.7e-3 by itself), features have one term, whose errors average over
 // them, and the weights P and the state, whose errors would add to it, two.
-// Projections take W in three terms (two for bf16 results): an error of the
-// exponent is one of phi.  All sums are fp32.
+// Projections take W in three terms (two for bf16 results) and bf16 rows as
+// they are: an error of the exponent is one of phi.  fp32 rows, brought below 1
+// by a power of two, and W are two fp16 terms, 2^-23 of an element each, and
+// three products (|W| < 65504).  All sums are fp32.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -59,7 +61,7 @@ __device__ __forceinline__ float decay(float rl, int dist) { return __builtin_am
 
 // ---- rows of x as operands
 template <typename TX>
-constexpr int kTermsX = sizeof(TX) == 2 ? 1 : 3;
+constexpr int kTermsX = sizeof(TX) == 2 ? 1 : 2;
 
 // Reads of rows of d elements through a buffer resource: offsets are in bytes from `base`, and what
 // lies at `bytes` or beyond (kOut among it) reads as zero.
@@ -161,14 +163,16 @@ struct Raw8 {
       for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(w[j]);
     }
   }
-  // the operand's terms (bf16: the elements themselves)
-  __device__ __forceinline__ void terms(uint4 (&t)[kTermsX<TX>]) const {
+  // the operand's terms (bf16: the elements themselves; fp32: those of scale times them)
+  __device__ __forceinline__ void terms(float scale, uint4 (&t)[kTermsX<TX>]) const {
     if constexpr (sizeof(TX) == 2) {
       t[0] = u[0];
     } else {
       float v[8];
       values(v);
-      split_bf16x8(v, t);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] *= scale;
+      split_f16x8(v, kLoScale, t[0], t[1]);
     }
   }
 };
@@ -200,9 +204,10 @@ __device__ __forceinline__ Sq<TX> row_square(const Raw8<TX> (&x)[DK]) {
   return s + __shfl_xor(s, 32);
 }
 
-// What phi takes of a row: PRF phi_prf's r, c, f (features.hpp); elu + 1: the row's scale and 1.
+// What phi takes of a row: PRF phi_prf's r, c, f (features.hpp); elu + 1: the row's scale and 1; x: what
+// its operand's terms were scaled by (fp32 rows: a power of two that brings them below 1).
 struct RowFactors {
-  float r, c, f;
+  float r, c, f, x;
 };
 template <bool ELU, typename S>
 __device__ __forceinline__ RowFactors row_factors(S sq, bool nprf, double log2_m) {
@@ -210,7 +215,13 @@ __device__ __forceinline__ RowFactors row_factors(S sq, bool nprf, double log2_m
   S scale = 1;
   if (nprf) scale = nz ? S(1) / sqrt(sq) : S(0);
   RowFactors o;
-  o.f = 1.f;
+  o.f = o.x = 1.f;
+  if constexpr (sizeof(S) == 8) {
+    const unsigned n = __float_as_uint(sqrtf(static_cast<float>(sq))) >> 23;  // |x| < 2^(n - 126)
+    const unsigned e = nz ? min(max(n, 2u), 252u) : 126u;
+    o.x = __uint_as_float((253u - e) << 23);
+    scale *= static_cast<S>(__uint_as_float((e + 1u) << 23));
+  }
   if constexpr (ELU) {
     o.r = static_cast<float>(scale), o.c = 0.f;
   } else {
@@ -220,10 +231,11 @@ __device__ __forceinline__ RowFactors row_factors(S sq, bool nprf, double log2_m
   }
   return o;
 }
-// WHOLE: the projection in two accumulators and the exponent's rounding made good (fp32 rows).
+// WHOLE: the projection in two accumulators, lo in units of 2^-11, and the exponent's rounding made
+// good (fp32 rows).
 template <bool ELU, bool WHOLE>
 __device__ __forceinline__ float feature(float s, float sl, float r, float c, float f) {
-  if constexpr (WHOLE) s += sl;
+  if constexpr (WHOLE) s = fmaf(sl, kLoInv, s);
   if constexpr (ELU) {
     const float x = s * r;
     return (x > 0.f ? x + 1.f : __builtin_amdgcn_exp2f(x * 1.44269504f)) * f;
@@ -251,7 +263,20 @@ __device__ __forceinline__ void load_weights(const Rows<float>& W, int f, int c,
     for (int t = 0; t < 4; ++t) v[4 + t] = u[t];
   }
 }
-template <int DK, int NW, bool ELU>
+// Eight of its elements as operand terms: NW bf16 ones, or (WHOLE) two fp16 ones.
+template <int NW, bool WHOLE>
+__device__ __forceinline__ void weight_terms(const float (&v)[8], uint4 (&t)[NW]) {
+  if constexpr (WHOLE) {
+    static_assert(NW == 2, "two fp16 terms");
+    split_f16x8(v, kLoScale, t[0], t[1]);
+  } else {
+    uint4 t3[3];
+    split_bf16x8(v, t3);
+#pragma unroll
+    for (int s = 0; s < NW; ++s) t[s] = t3[s];
+  }
+}
+template <int DK, int NW, bool ELU, bool WHOLE>
 struct WeightTile {
   static constexpr int N = 32 * 2 * DK / 256 > 0 ? 32 * 2 * DK / 256 : 1;
   float v[N][8];
@@ -268,37 +293,40 @@ struct WeightTile {
     for (int i = 0; i < N; ++i) {
       const int e = threadIdx.x + 256 * i, fl = e / (2 * DK), c = e % (2 * DK);
       if (DK * 64 < 256 && fl >= 32) return;
-      uint4 t3[3];
-      split_bf16x8(v[i], t3);
+      uint4 t[NW];
+      weight_terms<NW, WHOLE>(v[i], t);
       uint4* __restrict__ o = wf + (c >> 1) * NW * kFragLanes + (c & 1) * 32 + fl;
 #pragma unroll
-      for (int s = 0; s < NW; ++s) o[s * kFragLanes] = t3[s];
+      for (int s = 0; s < NW; ++s) o[s * kFragLanes] = t[s];
     }
   }
 };
 
-// Projections of 32 rows on 32 features: with WHOLE the products of the largest terms (acc) and
-// the others (lo) apart, else in one sum, the small ones first.
-template <int DK, int NSX, int NW, bool XROWS, bool WHOLE, typename F>
-__device__ __forceinline__ void project_terms(F&& weights, const uint4 (&xf)[DK][NSX], floatx16& acc, floatx16& lo) {
+// Projections of 32 rows on 32 features: with WHOLE h h (acc) and h l + l h (lo, in units of 2^-11)
+// apart, else all products of bf16 terms in one sum, the small ones first.
+template <int DK, int NSX, int NW, bool XROWS, bool WHOLE, typename FW, typename FX>
+__device__ __forceinline__ void project_terms(FW&& weights, FX&& rows, floatx16& acc, floatx16& lo) {
   acc = zero16();
   if constexpr (WHOLE) lo = zero16();
-  auto mul = [](uint4 w, uint4 x, floatx16 c) { return XROWS ? mfma_bf16(x, w, c) : mfma_bf16(w, x, c); };
+  auto mul = [](uint4 w, uint4 x, floatx16 c) {
+    if constexpr (WHOLE)
+      return XROWS ? mfma_f16(x, w, c) : mfma_f16(w, x, c);
+    else
+      return XROWS ? mfma_bf16(x, w, c) : mfma_bf16(w, x, c);
+  };
 #pragma unroll
   for (int ks = 0; ks < DK; ++ks) {
-    uint4 w[NW];
+    uint4 w[NW], x[NSX];
     weights(ks, w);
+    rows(ks, x);
+    if constexpr (WHOLE) {
+      lo = mul(w[0], x[1], lo);
+      lo = mul(w[1], x[0], lo);
+    } else {
 #pragma unroll
-    for (int s = 2; s >= 1; --s)
-#pragma unroll
-      for (int i = 0; i <= s; ++i)
-        if (i < NW && s - i < NSX) {
-          if constexpr (WHOLE)
-            lo = mul(w[i], xf[ks][s - i], lo);
-          else
-            acc = mul(w[i], xf[ks][s - i], acc);
-        }
-    acc = mul(w[0], xf[ks][0], acc);
+      for (int s = NW - 1; s >= 1; --s) acc = mul(w[s], x[0], acc);
+    }
+    acc = mul(w[0], x[0], acc);
   }
 }
 

@@ -124,10 +124,10 @@ template <typename TX, int DK, int NT, int SIDE, bool ELU>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k_decay_grad(DecayArgs a) {
   using TG = typename std::conditional<SIDE == 0, TX, float>::type;  // values of the other rows: v, or g
   constexpr bool WHOLE = sizeof(TX) == 4;
-  constexpr int NSX = kTermsX<TX>, DT = DK / 2, NW = 3;
+  constexpr int NSX = kTermsX<TX>, DT = DK / 2, NW = WHOLE ? 2 : 3;
   extern __shared__ __align__(16) uint4 smem[];
   // first pass                                        second pass
-  uint4* const wl = smem;                           // wl   [DK][3][64]
+  uint4* const wl = smem;                           // wl   [DK][NW][64]
   uint4* const kl = wl + DK * NW * kFragLanes;      // kl   [4][2][NT][64]
   uint4* const sl = kl + 8 * NT * kFragLanes;       // sl   [DT][2][NT][64]; then [DK][NT][64]
   uint4* const tl = sl + DK * NT * kFragLanes;      // tl   [DT][2][NT][64]
@@ -159,7 +159,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k
     const int dist = SIDE == 0 ? i - j : j - i;
     return dist >= 0 ? decay(rl, dist) : 0.f;
   };
-  WeightTile<DK, NW, ELU> wt;
+  WeightTile<DK, NW, ELU, WHOLE> wt;
   uint4 of[DK][NSX], tf[DK][NSX];
   RowFactors fo, ft;
   {
@@ -169,8 +169,16 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k
     fo = row_factors<ELU>(row_square<TX, DK>(x), a.nprf, a.log2_m);
     ft = row_factors<ELU>(row_square<TX, DK>(y), a.nprf, a.log2_m);
 #pragma unroll
-    for (int ks = 0; ks < DK; ++ks) x[ks].terms(of[ks]), y[ks].terms(tf[ks]);
+    for (int ks = 0; ks < DK; ++ks) x[ks].terms(fo.x, of[ks]), y[ks].terms(ft.x, tf[ks]);
   }
+  auto own_rows = [&](int ks, uint4(&x)[NSX]) {
+#pragma unroll
+    for (int n = 0; n < NSX; ++n) x[n] = of[ks][n];
+  };
+  auto other_rows = [&](int ks, uint4(&x)[NSX]) {
+#pragma unroll
+    for (int n = 0; n < NSX; ++n) x[n] = tf[ks][n];
+  };
   auto weights = [&](int ks, uint4(&w)[NW]) { read_terms<NW>(wl + ks * NW * kFragLanes, w); };
   // [g | gd] of the lane's row (SIDE 0), or its values (SIDE 1)
   floatx16 G[DT];
@@ -197,7 +205,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k
       __syncthreads();
       floatx16 acc, lo, ph;
       const bool part = f0 + 32 > a.M;
-      project_terms<DK, NSX, NW, false, WHOLE>(weights, tf, acc, lo);
+      project_terms<DK, NSX, NW, false, WHOLE>(weights, other_rows, acc, lo);
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         ph[e] = feature<ELU, WHOLE>(acc[e], WHOLE ? lo[e] : 0.f, ft.r, ft.c, ft.f);
@@ -210,7 +218,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k
 #pragma unroll
         for (int s = 0; s < NT; ++s) kl[((wave * 2 + k2) * NT + s) * kFragLanes + lane] = t[s];
       }
-      project_terms<DK, NSX, NW, false, WHOLE>(weights, of, acc, lo);
+      project_terms<DK, NSX, NW, false, WHOLE>(weights, own_rows, acc, lo);
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         ph[e] = feature<ELU, WHOLE>(acc[e], WHOLE ? lo[e] : 0.f, fo.r, fo.c, fo.f);
@@ -375,7 +383,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k
     __syncthreads();
     floatx16 acc, lo, ph, df = zero16();
     // features of the other rows with the positions along the registers: their factors by lane
-    project_terms<DK, NSX, NW, true, WHOLE>(weights, tf, acc, lo);
+    project_terms<DK, NSX, NW, true, WHOLE>(weights, other_rows, acc, lo);
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
       const int from = 8 * (e >> 2) + 4 * lh + (e & 3);  // the lane that holds this row's factors
@@ -399,7 +407,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k
 #pragma unroll
       for (int e = 0; e < 16; ++e) df[e] = fmaf(sden[8 * (e >> 2) + 4 * lh + (e & 3)], one, df[e]);
     }
-    project_terms<DK, NSX, NW, false, WHOLE>(weights, of, acc, lo);
+    project_terms<DK, NSX, NW, false, WHOLE>(weights, own_rows, acc, lo);
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
       const int l = 8 * (e >> 2) + 4 * lh + (e & 3);
@@ -442,7 +450,7 @@ namespace {
 template <typename TX, int DK, bool ELU>
 hipError_t go(const DecayArgs& a, hipStream_t st) {
   constexpr int NT = sizeof(TX) == 2 ? 2 : 3, NV = sizeof(TX) == 2 ? 1 : 3, DT = DK / 2;
-  constexpr int loop = DK * 3 + 8 * NT + DK * NT + DT * 2 * NT, mid = 4 * DK * NT;
+  constexpr int loop = DK * (sizeof(TX) == 2 ? 3 : 2) + 8 * NT + DK * NT + DT * 2 * NT, mid = 4 * DK * NT;
   constexpr int lds = (loop > mid ? loop : mid) * 1024;
   if constexpr (lds > 65536) {
     (void)hipFuncSetAttribute(reinterpret_cast<const void*>(&k_decay_grad<TX, DK, NT, 0, ELU>),

@@ -17,13 +17,15 @@ namespace krpe {
 // while those at hand are worked on.
 // NT: terms of features and values; NP: of P and the state.
 template <typename TX, int DK, int NT, int NP, bool ELU>
-__global__ __launch_bounds__(256, sizeof(TX) == 2 && DK <= 4 ? 2 : 1) void k_decay_out(DecayArgs a) {
+__global__ __launch_bounds__(256, DK <= 4 ? 2 : 1) void k_decay_out(DecayArgs a) {
   constexpr bool WHOLE = sizeof(TX) == 4;
-  constexpr int NSX = kTermsX<TX>, DT = DK / 2, NW = WHOLE ? 3 : 2;
+  constexpr int NSX = kTermsX<TX>, DT = DK / 2, NW = 2;
+  constexpr bool KROWS = WHOLE;  // the rows of k through LDS, where registers are short
   extern __shared__ __align__(16) uint4 smem[];
   uint4* const wl = smem;                            // [DK][NW][64]
   uint4* const sl = wl + DK * NW * kFragLanes;       // [DT][2][NP][64]
   uint4* const kl = sl + DT * 2 * NP * kFragLanes;   // [4][2][NT][64]
+  uint4* const xl = kl + 8 * NT * kFragLanes;        // KROWS: k [4][DK][NSX][64], each wave its own
   uint4* const vl = smem;                            // [4][DT][2][NT][64], after the features
   __shared__ __align__(16) float sden[32];
   __shared__ int odd;
@@ -47,10 +49,10 @@ __global__ __launch_bounds__(256, sizeof(TX) == 2 && DK <= 4 ? 2 : 1) void k_dec
   const size_t from = base + static_cast<size_t>(p0) * d;
   const Rows<TX> qr(static_cast<const TX*>(a.q) + from, cnt, d), kr(static_cast<const TX*>(a.k) + from, cnt, d),
       vr(static_cast<const TX*>(a.v) + from, cnt, d);
-  WeightTile<DK, NW, ELU> wt;
+  WeightTile<DK, NW, ELU, WHOLE> wt;
   wt.fetch(W, 0);
   state.fetch(0);
-  uint4 qf[DK][NSX], kf[DK][NSX];
+  uint4 qf[DK][NSX], kf[KROWS ? 1 : DK][NSX];
   RowFactors fq, fk;
   {
     Raw8<TX> x[DK], y[DK];
@@ -59,7 +61,17 @@ __global__ __launch_bounds__(256, sizeof(TX) == 2 && DK <= 4 ? 2 : 1) void k_dec
     fq = row_factors<ELU>(row_square<TX, DK>(x), a.nprf, a.log2_m);
     fk = row_factors<ELU>(row_square<TX, DK>(y), a.nprf, a.log2_m);
 #pragma unroll
-    for (int ks = 0; ks < DK; ++ks) x[ks].terms(qf[ks]), y[ks].terms(kf[ks]);
+    for (int ks = 0; ks < DK; ++ks) {
+      x[ks].terms(fq.x, qf[ks]);
+      if constexpr (KROWS) {
+        uint4 t[NSX];
+        y[ks].terms(fk.x, t);
+#pragma unroll
+        for (int n = 0; n < NSX; ++n) xl[((wave * DK + ks) * NSX + n) * kFragLanes + lane] = t[n];
+      } else {
+        y[ks].terms(fk.x, kf[ks]);
+      }
+    }
   }
   floatx16 S[4], Z[DT];
 #pragma unroll
@@ -81,8 +93,8 @@ __global__ __launch_bounds__(256, sizeof(TX) == 2 && DK <= 4 ? 2 : 1) void k_dec
     __syncthreads();
     floatx16 acc, lo, ph;
     const bool part = f0 + 32 > a.M;  // uniform: features past M weigh nothing
-    auto features = [&](const uint4(&xf)[DK][NSX], const RowFactors& o) {
-      project_terms<DK, NSX, NW, false, WHOLE>(weights, xf, acc, lo);
+    auto features = [&](auto&& rows, const RowFactors& o) {
+      project_terms<DK, NSX, NW, false, WHOLE>(weights, rows, acc, lo);
 #pragma unroll
       for (int e = 0; e < 16; ++e) ph[e] = feature<ELU, WHOLE>(acc[e], WHOLE ? lo[e] : 0.f, o.r, o.c, o.f);
       if (part) {
@@ -91,7 +103,16 @@ __global__ __launch_bounds__(256, sizeof(TX) == 2 && DK <= 4 ? 2 : 1) void k_dec
           if (f0 + 8 * (e >> 2) + 4 * lh + (e & 3) >= a.M) ph[e] = 0.f;
       }
     };
-    features(kf, fk);
+    features(
+        [&](int ks, uint4(&x)[NSX]) {
+          if constexpr (KROWS) {
+            read_terms<NSX>(xl + (wave * DK + ks) * NSX * kFragLanes, x);
+          } else {
+#pragma unroll
+            for (int n = 0; n < NSX; ++n) x[n] = kf[ks][n];
+          }
+        },
+        fk);
 #pragma unroll
     for (int k2 = 0; k2 < 2; ++k2) {
       uint4 t[NT];
@@ -99,7 +120,12 @@ __global__ __launch_bounds__(256, sizeof(TX) == 2 && DK <= 4 ? 2 : 1) void k_dec
 #pragma unroll
       for (int s = 0; s < NT; ++s) kl[((wave * 2 + k2) * NT + s) * kFragLanes + lane] = t[s];
     }
-    features(qf, fq);
+    features(
+        [&](int ks, uint4(&x)[NSX]) {
+#pragma unroll
+          for (int n = 0; n < NSX; ++n) x[n] = qf[ks][n];
+        },
+        fq);
     uint4 pq[2][NT];
     pack_half<NT>(ph, 0, pq[0]);
     pack_half<NT>(ph, 1, pq[1]);
@@ -209,8 +235,8 @@ hipError_t go(const DecayArgs& a, hipStream_t st) {
   // (a single chunk from zeros whose state is not kept needs no sums)
   if (a.state || a.nchunk > 1) launch_decay_states<TX, TX, DK, 3, NT, ELU, Sums::kForth>(a, st);
   if (a.nchunk > 0) {
-    constexpr int NW = NT == 1 ? 2 : 3;
-    constexpr int feat = DK * NW + DT * 2 * NP + 8 * NT, vals = 8 * DT * NT;
+    constexpr int NSX = kTermsX<TX>, NW = 2;
+    constexpr int feat = DK * NW + DT * 2 * NP + 8 * NT + (sizeof(TX) == 4 ? 4 * DK * NSX : 0), vals = 8 * DT * NT;
     constexpr int lds = (feat > vals ? feat : vals) * 1024;
     if constexpr (lds > 65536)
       (void)hipFuncSetAttribute(reinterpret_cast<const void*>(&k_decay_out<TX, DK, NT, NP, ELU>),

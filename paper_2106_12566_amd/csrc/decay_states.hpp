@@ -33,7 +33,7 @@ __device__ __forceinline__ int path_rows(const int* __restrict__ path, int P, in
 template <typename TX, typename TV, int DK, int NP, int NV, bool ELU, Sums MODE, int WAVES>
 __global__ __launch_bounds__(64 * WAVES, DK <= 4 ? 2 : 1) void k_decay_states(DecayArgs a) {
   constexpr bool BACK = MODE == Sums::kBack, PATH = MODE == Sums::kPath, WHOLE = sizeof(TX) == 4;
-  constexpr int NSX = kTermsX<TX>, DT = DK / 2, PB = WHOLE || DK == 8 || PATH ? 2 : 4;
+  constexpr int NSX = kTermsX<TX>, NW = WHOLE ? 2 : 3, DT = DK / 2, PB = WHOLE || DK == 8 || PATH ? 2 : 4;
   constexpr int BPW = (PB + WAVES - 1) / WAVES;  // blocks of x that a wave stages
   __shared__ __align__(16) uint4 xl[PB * DK * NSX * kFragLanes], vl[PB * DT * 2 * NV * kFragLanes];
   __shared__ __align__(16) float fr[32 * PB], fc[32 * PB], ff[32 * PB], fd[BACK ? 32 * PB : 4];
@@ -77,14 +77,14 @@ __global__ __launch_bounds__(64 * WAVES, DK <= 4 ? 2 : 1) void k_decay_states(De
       return PATH && at < 0 ? kOut : vr.at(at);
     });
   };
-  uint4 wf[DK][3];
+  uint4 wf[DK][NW];
   {
     const Rows<float> W(a.W + static_cast<size_t>(h) * M * d, M, d);
 #pragma unroll
     for (int ks = 0; ks < DK; ++ks) {
       float v8[8];
       load_weights<ELU>(W, l, 16 * ks + 8 * lh, v8);
-      split_bf16x8(v8, wf[ks]);
+      weight_terms<NW, WHOLE>(v8, wf[ks]);
     }
   }
   floatx16 S[DT];
@@ -130,18 +130,17 @@ __global__ __launch_bounds__(64 * WAVES, DK <= 4 ? 2 : 1) void k_decay_states(De
       for (int i = 0; i < BPW; ++i) {
         const int blk = wave + WAVES * i;
         if (blk < PB) {
-          const Sq<TX> sq = row_square<TX, DK>(rx[i]);
+          RowFactors o = row_factors<ELU>(row_square<TX, DK>(rx[i]), a.nprf, a.log2_m);
 #pragma unroll
           for (int ks = 0; ks < DK; ++ks) {
             uint4 t[NSX];
-            rx[i][ks].terms(t);
+            rx[i][ks].terms(o.x, t);
 #pragma unroll
             for (int n = 0; n < NSX; ++n) xl[((blk * DK + ks) * NSX + n) * kFragLanes + lane] = t[n];
           }
           if (lh == 0) {
             // the weight of the chunk's end, e^{-rate (cnt - 1 - r)}, goes with the row's factors
             const int r = q0 + 32 * blk + lr;
-            RowFactors o = row_factors<ELU>(sq, a.nprf, a.log2_m);
             const float e = -rl * static_cast<float>(BACK ? r : cnt - 1 - r);
             if constexpr (ELU)
               o.f = r < cnt ? __builtin_amdgcn_exp2f(e) : 0.f;
@@ -169,16 +168,13 @@ __global__ __launch_bounds__(64 * WAVES, DK <= 4 ? 2 : 1) void k_decay_states(De
       }
 #pragma unroll 1
       for (int blk = 0; blk < PB && q0 + 32 * blk < cnt; ++blk) {
-        uint4 xf[DK][NSX];
-#pragma unroll
-        for (int ks = 0; ks < DK; ++ks) read_terms<NSX>(xl + (blk * DK + ks) * NSX * kFragLanes, xf[ks]);
         floatx16 acc, lo, ph;
-        project_terms<DK, NSX, 3, true, WHOLE>(
-            [&](int ks, uint4(&w)[3]) {
+        project_terms<DK, NSX, NW, true, WHOLE>(
+            [&](int ks, uint4(&w)[NW]) {
 #pragma unroll
-              for (int n = 0; n < 3; ++n) w[n] = wf[ks][n];
+              for (int n = 0; n < NW; ++n) w[n] = wf[ks][n];
             },
-            xf, acc, lo);
+            [&](int ks, uint4(&x)[NSX]) { read_terms<NSX>(xl + (blk * DK + ks) * NSX * kFragLanes, x); }, acc, lo);
 #pragma unroll
         for (int g = 0; g < 4; ++g) {
           const int at = 32 * blk + 8 * g + 4 * lh;

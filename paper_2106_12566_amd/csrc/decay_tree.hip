@@ -25,7 +25,7 @@ template <typename TX, int DK, int NT, int NPP, int RT, bool ELU>
 __global__ __launch_bounds__(64 * kSplit * RT, sizeof(TX) == 2 && DK <= 4 ? 2 : 1) void k_decay_tree(PoolArgs a) {
   constexpr bool WHOLE = sizeof(TX) == 4;
   constexpr int THREADS = 64 * kSplit * RT, NX = sizeof(TX) / 2;
-  constexpr int NSX = kTermsX<TX>, DT = DK / 2, NW = WHOLE ? 3 : 2, NP = RT == 1 ? 1 : 3;
+  constexpr int NSX = kTermsX<TX>, DT = DK / 2, NW = 2, NP = RT == 1 ? 1 : 3;
   constexpr int CG = DT < 2 ? DT : 2;  // column tiles summed at a time
   // first the rows as they are [k, q][RT][DK][NX][64]; then the partial sums: S tiles [kSplit][NP], Z
   // [kSplit][RT][CG] a group of columns at a time
@@ -36,7 +36,7 @@ __global__ __launch_bounds__(64 * kSplit * RT, sizeof(TX) == 2 && DK <= 4 ? 2 : 
   __shared__ __align__(16) uint4 pl[NP][2][NPP][64];  // P as operands
   __shared__ __align__(16) uint4 vl[RT * DT * 2 * NT * 64];
   __shared__ float dpart[kSplit][32 * RT], dsum[NP][32];
-  __shared__ float fr[2][32 * RT], fc[2][32 * RT], ff[2][32 * RT];
+  __shared__ float fr[2][32 * RT], fc[2][32 * RT], ff[2][32 * RT], fx[2][32 * RT];
   __shared__ unsigned long long seen[32 * RT];
   __shared__ int odd;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -135,7 +135,7 @@ __global__ __launch_bounds__(64 * kSplit * RT, sizeof(TX) == 2 && DK <= 4 ? 2 : 
       if (stages) {
         const RowFactors o = row_factors<ELU>(row_square<TX, DK>(raw), a.nprf, a.log2_m);
         const int w = wave & 1, t = wave >> 1;
-        if (lh == 0) fr[w][32 * t + lr] = o.r, fc[w][32 * t + lr] = o.c, ff[w][32 * t + lr] = o.f;
+        if (lh == 0) fr[w][32 * t + lr] = o.r, fc[w][32 * t + lr] = o.c, ff[w][32 * t + lr] = o.f, fx[w][32 * t + lr] = o.x;
 #pragma unroll
         for (int ks = 0; ks < DK; ++ks)
 #pragma unroll
@@ -146,28 +146,22 @@ __global__ __launch_bounds__(64 * kSplit * RT, sizeof(TX) == 2 && DK <= 4 ? 2 : 
     }
     uint4 wf[DK][NW];
 #pragma unroll
-    for (int ks = 0; ks < DK; ++ks) {
-      uint4 t3[3];
-      split_bf16x8(w8[ks], t3);
-#pragma unroll
-      for (int s = 0; s < NW; ++s) wf[ks][s] = t3[s];
-    }
+    for (int ks = 0; ks < DK; ++ks) weight_terms<NW, WHOLE>(w8[ks], wf[ks]);
     // features of a row tile (lane: row; features along the registers), zeros past M
     auto features = [&](int w, int t, floatx16& ph, uint4(&p)[2][NT]) {
-      uint4 xf[DK][NSX];
-#pragma unroll
-      for (int ks = 0; ks < DK; ++ks) {
-        Raw8<TX> x;
-        read_terms<NX>(xl + ((w * RT + t) * DK + ks) * NX * 64, x.u);
-        x.terms(xf[ks]);
-      }
+      const float scale = fx[w][32 * t + lr];
       floatx16 acc, lo;
       project_terms<DK, NSX, NW, false, WHOLE>(
           [&](int ks, uint4(&y)[NW]) {
 #pragma unroll
             for (int n = 0; n < NW; ++n) y[n] = wf[ks][n];
           },
-          xf, acc, lo);
+          [&](int ks, uint4(&y)[NSX]) {
+            Raw8<TX> x;
+            read_terms<NX>(xl + ((w * RT + t) * DK + ks) * NX * 64, x.u);
+            x.terms(scale, y);
+          },
+          acc, lo);
       const float r_ = fr[w][32 * t + lr], c_ = fc[w][32 * t + lr], f_ = ff[w][32 * t + lr];
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
