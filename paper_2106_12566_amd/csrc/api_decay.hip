@@ -23,15 +23,21 @@ DecayLayout decay_layout(long long BH, int n, int d, int m, size_t off) {
   DecayLayout L{};
   L.Mp = (m + 31) & ~31;
   L.nchunk = (n + kChunk - 1) / kChunk;
-  // enough work-groups (128 features each) for three on a CU; a segment more costs a state
+  // The number of segments from the rounds of work-groups that the sums take: a group of 128
+  // features and a segment each, two to a CU (one beyond 64 dimensions, twice as many of the
+  // two-wave groups of up to 64 features), a chunk costing one unit, a group's start a half and
+  // the state of a segment, written and joined, a twentieth.  (16 heads of 256 features, 128 chunks: 22
+  // segments, in two rounds, 117 us, 16 in one 85; 8 x 12 heads, 32 chunks: 8 in two rounds 127, 5 in one 131.)
   const long long groups = BH * ((L.Mp + 127) / 128);
-  long long nseg = groups > 0 ? (768 + groups - 1) / groups : 1;
-  if (nseg > L.nchunk) nseg = L.nchunk;
-  if (nseg < 1) nseg = 1;
-  L.segc = static_cast<int>((L.nchunk + nseg - 1) / nseg);
-  if (L.segc < 1) L.segc = 1;
-  L.nseg = (L.nchunk + L.segc - 1) / L.segc;
-  if (L.nseg < 1) L.nseg = 1;
+  const long long slots = (d <= 64 ? 512 : 256) * (L.Mp <= 64 ? 2 : 1);
+  double best = 0.0;
+  L.nseg = 1, L.segc = L.nchunk > 1 ? L.nchunk : 1;
+  for (int segc = L.nchunk; segc >= 1; --segc) {
+    const int nseg = (L.nchunk + segc - 1) / segc;
+    if (nseg > 256) break;
+    const double cost = static_cast<double>((groups * nseg + slots - 1) / slots) * (segc + 0.5) + 0.05 * nseg;
+    if (segc == L.nchunk || cost < best) best = cost, L.nseg = nseg, L.segc = segc;
+  }
   const size_t cells = static_cast<size_t>(d + 1) * L.Mp * sizeof(float);
   L.tot = off;
   L.pre = align_up(L.tot + BH * L.nseg * cells);

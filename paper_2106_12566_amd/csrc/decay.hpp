@@ -59,6 +59,40 @@ __device__ __forceinline__ int slot_of(const int* __restrict__ slots, int b, int
 __device__ __forceinline__ float rate_log2(float rate) { return (rate > 1e6f ? 1e6f : rate) * 1.44269504f; }
 __device__ __forceinline__ float decay(float rl, int dist) { return __builtin_amdgcn_exp2f(-rl * static_cast<float>(dist)); }
 
+// The weights e^{-rate dist} of a 32 x 32 result's rows: dist = sign (i - j) for the lane's row i and rows
+// j = base + 8 (e / 4) + 4 lh + e % 4 along the registers; zero below 0 (EDGE: where that can be).
+// Where 32 positions keep 2^-60, as the product of the lane's weight and 16 others that all tiles share.
+struct TileWeights {
+  float rl;
+  bool near;  // uniform
+  float t[16];
+  int sign;
+  __device__ __forceinline__ TileWeights(float rl_, int sign_) : rl(rl_), near(fabsf(rl_) * 32.f < 60.f), sign(sign_) {
+    const int lh = (threadIdx.x & 63) >> 5;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) t[e] = decay(rl, -sign * (8 * (e >> 2) + 4 * lh + (e & 3)));
+  }
+  template <bool EDGE>
+  __device__ __forceinline__ void apply(floatx16& x, int i, int base) const {
+    const int lh = (threadIdx.x & 63) >> 5;
+    const int d0 = sign * (i - base);
+    if (near) {
+      const float w = decay(rl, d0);
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float y = x[e] * (w * t[e]);
+        x[e] = !EDGE || d0 - sign * (8 * (e >> 2) + 4 * lh + (e & 3)) >= 0 ? y : 0.f;
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int dist = d0 - sign * (8 * (e >> 2) + 4 * lh + (e & 3));
+        x[e] = dist >= 0 ? x[e] * decay(rl, dist) : 0.f;
+      }
+    }
+  }
+};
+
 // ---- rows of x as operands
 template <typename TX>
 constexpr int kTermsX = sizeof(TX) == 2 ? 1 : 2;
@@ -183,65 +217,53 @@ __device__ __forceinline__ void fetch_row(const Rows<TX>& rows, uint32_t o, Raw8
 #pragma unroll
   for (int ks = 0; ks < DK; ++ks) x[ks].load(rows, o, 16 * ks + 8 * lh);
 }
-// Its squared norm: in fp64 for fp32 rows, whose features are held whole; for bf16 ones in fp32,
-// in eight partial sums a lane (off by a few 2^-24 of itself).
-template <typename TX>
-using Sq = typename std::conditional<sizeof(TX) == 2, float, double>::type;
+// Its squared norm, in eight partial sums a lane (off by a few 2^-25 of itself: at the sizes where
+// features stay in range that is less than the rounding of the exponent).
 template <typename TX, int DK>
-__device__ __forceinline__ Sq<TX> row_square(const Raw8<TX> (&x)[DK]) {
-  Sq<TX> p[8] = {};
+__device__ __forceinline__ float row_square(const Raw8<TX> (&x)[DK]) {
+  float p[8] = {};
 #pragma unroll
   for (int ks = 0; ks < DK; ++ks) {
     float v[8];
     x[ks].values(v);
 #pragma unroll
-    for (int t = 0; t < 8; ++t) {
-      const Sq<TX> y = v[t];
-      p[t] = fma(y, y, p[t]);
-    }
+    for (int t = 0; t < 8; ++t) p[t] = fmaf(v[t], v[t], p[t]);
   }
-  const Sq<TX> s = ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+  const float s = ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
   return s + __shfl_xor(s, 32);
 }
 
-// What phi takes of a row: PRF phi_prf's r, c, f (features.hpp); elu + 1: the row's scale and 1; x: what
-// its operand's terms were scaled by (fp32 rows: a power of two that brings them below 1).
+// What phi takes of a row: PRF 2^(s r + c) of the projection s, r = log2(e) (over ||x|| when
+// normalising), c = -||x||^2 / 2 log2(e) - log2(sqrt(m)); elu + 1 r alone.  x: what the operand's
+// terms were scaled by (fp32 rows: a power of two that brings them below 1, which r makes good).
 struct RowFactors {
-  float r, c, f, x;
+  float r, c, x;
 };
-template <bool ELU, typename S>
-__device__ __forceinline__ RowFactors row_factors(S sq, bool nprf, double log2_m) {
-  const bool nz = sq > 0;
-  S scale = 1;
-  if (nprf) scale = nz ? S(1) / sqrt(sq) : S(0);
+template <bool ELU, bool WHOLE>
+__device__ __forceinline__ RowFactors row_factors(float sq, bool nprf, double log2_m) {
+  const bool nz = sq > 0.f;
+  const float norm = sqrtf(sq);
   RowFactors o;
-  o.f = o.x = 1.f;
-  if constexpr (sizeof(S) == 8) {
-    const unsigned n = __float_as_uint(sqrtf(static_cast<float>(sq))) >> 23;  // |x| < 2^(n - 126)
+  o.r = (ELU ? 1.f : static_cast<float>(kLog2e)) * (nprf ? (nz ? 1.f / norm : 0.f) : 1.f);
+  o.c = static_cast<float>(log2_m) - (nprf ? (nz ? 0.5f : 0.f) : 0.5f * sq) * static_cast<float>(kLog2e);
+  o.x = 1.f;
+  if constexpr (WHOLE) {
+    const unsigned n = __float_as_uint(norm) >> 23;  // |x| < 2^(n - 126)
     const unsigned e = nz ? min(max(n, 2u), 252u) : 126u;
     o.x = __uint_as_float((253u - e) << 23);
-    scale *= static_cast<S>(__uint_as_float((e + 1u) << 23));
-  }
-  if constexpr (ELU) {
-    o.r = static_cast<float>(scale), o.c = 0.f;
-  } else {
-    const S c = static_cast<S>(log2_m) - (nprf ? (nz ? S(0.5) : S(0)) : S(0.5) * sq) * static_cast<S>(kLog2e);
-    o.r = static_cast<float>(scale * static_cast<S>(kLog2e)), o.c = static_cast<float>(c);
-    if constexpr (sizeof(S) == 8) o.f = rounding_factor(c, o.c);
+    o.r *= __uint_as_float((e + 1u) << 23);
   }
   return o;
 }
-// WHOLE: the projection in two accumulators, lo in units of 2^-11, and the exponent's rounding made
-// good (fp32 rows).
+// WHOLE: the projection in two accumulators, lo in units of 2^-11 (fp32 rows).
 template <bool ELU, bool WHOLE>
-__device__ __forceinline__ float feature(float s, float sl, float r, float c, float f) {
+__device__ __forceinline__ float feature(float s, float sl, float r, float c) {
   if constexpr (WHOLE) s = fmaf(sl, kLoInv, s);
   if constexpr (ELU) {
     const float x = s * r;
-    return (x > 0.f ? x + 1.f : __builtin_amdgcn_exp2f(x * 1.44269504f)) * f;
+    return x > 0.f ? x + 1.f : __builtin_amdgcn_exp2f(x * 1.44269504f);
   } else {
-    const float y = __builtin_amdgcn_exp2f(fmaf(s, r, c));
-    return WHOLE ? y * f : y;
+    return __builtin_amdgcn_exp2f(fmaf(s, r, c));
   }
 }
 

@@ -147,17 +147,22 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k
   const float* __restrict__ old =
       a.nseg > 1 ? (SIDE == 0 ? a.tot : a.totb) + (static_cast<size_t>(bh) * a.nseg + seg) * cells : nullptr;
   const float wold = decay(rl, SIDE == 0 ? (ch - c0) * kChunk : min(rows, c1 * kChunk) - (p0 + cnt));
-  const int i = 32 * wave + lr;  // the lane's own row
+  // the row tile of a wave: those with the most to do the other way round in every other 256
+  // work-groups, which share a CU
+  const int rt = (blockIdx.x >> 8) & 1 ? 3 - wave : wave;
+  const int i = 32 * rt + lr;  // the lane's own row
   const float share = decay(rl, SIDE == 0 ? i + 1 : cnt - min(i, cnt));  // of the state outside the chunk
   const size_t from = base + static_cast<size_t>(p0) * d;
   const Rows<TX> own(static_cast<const TX*>(SIDE == 0 ? a.q : a.k) + from, cnt, d);
   const Rows<TX> oth(static_cast<const TX*>(SIDE == 0 ? a.k : a.q) + from, cnt, d);
   const Rows<TG> vals((SIDE == 0 ? static_cast<const TG*>(a.v) : reinterpret_cast<const TG*>(a.g)) + from, cnt, d);
-  auto uses = [&](int t) { return SIDE == 0 ? t <= wave : t >= wave; };  // tiles of the other rows
-  auto weight = [&](int t, int e) {
-    const int j = 32 * t + 8 * (e >> 2) + 4 * lh + (e & 3);
-    const int dist = SIDE == 0 ? i - j : j - i;
-    return dist >= 0 ? decay(rl, dist) : 0.f;
+  auto uses = [&](int t) { return SIDE == 0 ? t <= rt : t >= rt; };  // tiles of the other rows
+  const TileWeights weights_of(rl, SIDE == 0 ? 1 : -1);
+  auto weigh = [&](floatx16& x, int t) {
+    if (t == rt)
+      weights_of.template apply<true>(x, i, 32 * t);
+    else
+      weights_of.template apply<false>(x, i, 32 * t);
   };
   WeightTile<DK, NW, ELU, WHOLE> wt;
   uint4 of[DK][NSX], tf[DK][NSX];
@@ -166,8 +171,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k
     Raw8<TX> x[DK], y[DK];
     fetch_row<TX, DK>(own, own.at(i), x);
     fetch_row<TX, DK>(oth, oth.at(i), y);
-    fo = row_factors<ELU>(row_square<TX, DK>(x), a.nprf, a.log2_m);
-    ft = row_factors<ELU>(row_square<TX, DK>(y), a.nprf, a.log2_m);
+    fo = row_factors<ELU, WHOLE>(row_square<TX, DK>(x), a.nprf, a.log2_m);
+    ft = row_factors<ELU, WHOLE>(row_square<TX, DK>(y), a.nprf, a.log2_m);
 #pragma unroll
     for (int ks = 0; ks < DK; ++ks) x[ks].terms(fo.x, of[ks]), y[ks].terms(ft.x, tf[ks]);
   }
@@ -208,7 +213,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k
       project_terms<DK, NSX, NW, false, WHOLE>(weights, other_rows, acc, lo);
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        ph[e] = feature<ELU, WHOLE>(acc[e], WHOLE ? lo[e] : 0.f, ft.r, ft.c, ft.f);
+        ph[e] = feature<ELU, WHOLE>(acc[e], WHOLE ? lo[e] : 0.f, ft.r, ft.c);
         if (part && f0 + 8 * (e >> 2) + 4 * lh + (e & 3) >= a.M) ph[e] = 0.f;
       }
 #pragma unroll
@@ -216,12 +221,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k
         uint4 t[NT];
         pack_half<NT>(ph, k2, t);
 #pragma unroll
-        for (int s = 0; s < NT; ++s) kl[((wave * 2 + k2) * NT + s) * kFragLanes + lane] = t[s];
+        for (int s = 0; s < NT; ++s) kl[((rt * 2 + k2) * NT + s) * kFragLanes + lane] = t[s];
       }
       project_terms<DK, NSX, NW, false, WHOLE>(weights, own_rows, acc, lo);
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        ph[e] = feature<ELU, WHOLE>(acc[e], WHOLE ? lo[e] : 0.f, fo.r, fo.c, fo.f);
+        ph[e] = feature<ELU, WHOLE>(acc[e], WHOLE ? lo[e] : 0.f, fo.r, fo.c);
         if (part && f0 + 8 * (e >> 2) + 4 * lh + (e & 3) >= a.M) ph[e] = 0.f;
       }
       uint4 po[2][NT];
@@ -266,10 +271,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k
 #pragma unroll
     for (int t = 0; t < 4; ++t)
       if (uses(t)) {
+        weigh(S[t], t);
+        if constexpr (SIDE == 0) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          S[t][e] *= weight(t, e);
-          if constexpr (SIDE == 0) den += S[t][e];
+          for (int e = 0; e < 16; ++e) den += S[t][e];
         }
 #pragma unroll
         for (int k2 = 0; k2 < 2; ++k2) {
@@ -346,8 +351,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         const float one = SIDE == 0 ? gd : sgd[32 * t + 8 * (e >> 2) + 4 * lh + (e & 3)];
-        r[e] = (r[e] + one) * weight(t, e);
+        r[e] += one;
       }
+      weigh(r, t);
       pack_half<NT>(r, 0, R[t][0]);
       pack_half<NT>(r, 1, R[t][1]);
     }
@@ -387,7 +393,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
       const int from = 8 * (e >> 2) + 4 * lh + (e & 3);  // the lane that holds this row's factors
-      ph[e] = feature<ELU, WHOLE>(acc[e], WHOLE ? lo[e] : 0.f, __shfl(ft.r, from), __shfl(ft.c, from), __shfl(ft.f, from));
+      ph[e] = feature<ELU, WHOLE>(acc[e], WHOLE ? lo[e] : 0.f, __shfl(ft.r, from), __shfl(ft.c, from));
     }
     if (f0 + lr >= a.M) ph = zero16();
 #pragma unroll
@@ -395,7 +401,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k
       uint4 t[NT];
       pack_half<NT>(ph, k2, t);
 #pragma unroll
-      for (int s = 0; s < NT; ++s) kl[((wave * 2 + k2) * NT + s) * kFragLanes + lane] = t[s];
+      for (int s = 0; s < NT; ++s) kl[((rt * 2 + k2) * NT + s) * kFragLanes + lane] = t[s];
     }
     if (state.any()) {
 #pragma unroll
@@ -411,7 +417,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
       const int l = 8 * (e >> 2) + 4 * lh + (e & 3);
-      ph[e] = feature<ELU, WHOLE>(acc[e], WHOLE ? lo[e] : 0.f, fo.r, fo.c, fo.f);
+      ph[e] = feature<ELU, WHOLE>(acc[e], WHOLE ? lo[e] : 0.f, fo.r, fo.c);
       if constexpr (ELU) ph[e] = fminf(ph[e], 1.f);  // the slope of elu + 1 is e^x below zero, 1 above
       if (f0 + l >= a.M) ph[e] = 0.f;
     }

@@ -45,7 +45,10 @@ __global__ __launch_bounds__(256, DK <= 4 ? 2 : 1) void k_decay_out(DecayArgs a)
   const float* __restrict__ old = whole ? nullptr : a.tot + (static_cast<size_t>(bh) * a.nseg + seg) * cells;
   StateTile<DT, NP, false> state(old, pre, decay(rl, inseg * kChunk), d, a.Mp);
   const bool has = state.any();
-  const int i = 32 * wave + lr;
+  // the row tile of a wave: the last ones have the most to do, so that every other 256 work-groups
+  // (those that share a CU) have them the other way round
+  const int rt = (blockIdx.x >> 8) & 1 ? 3 - wave : wave;
+  const int i = 32 * rt + lr;
   const size_t from = base + static_cast<size_t>(p0) * d;
   const Rows<TX> qr(static_cast<const TX*>(a.q) + from, cnt, d), kr(static_cast<const TX*>(a.k) + from, cnt, d),
       vr(static_cast<const TX*>(a.v) + from, cnt, d);
@@ -58,8 +61,8 @@ __global__ __launch_bounds__(256, DK <= 4 ? 2 : 1) void k_decay_out(DecayArgs a)
     Raw8<TX> x[DK], y[DK];
     fetch_row<TX, DK>(qr, qr.at(i), x);
     fetch_row<TX, DK>(kr, kr.at(i), y);
-    fq = row_factors<ELU>(row_square<TX, DK>(x), a.nprf, a.log2_m);
-    fk = row_factors<ELU>(row_square<TX, DK>(y), a.nprf, a.log2_m);
+    fq = row_factors<ELU, WHOLE>(row_square<TX, DK>(x), a.nprf, a.log2_m);
+    fk = row_factors<ELU, WHOLE>(row_square<TX, DK>(y), a.nprf, a.log2_m);
 #pragma unroll
     for (int ks = 0; ks < DK; ++ks) {
       x[ks].terms(fq.x, qf[ks]);
@@ -67,7 +70,7 @@ __global__ __launch_bounds__(256, DK <= 4 ? 2 : 1) void k_decay_out(DecayArgs a)
         uint4 t[NSX];
         y[ks].terms(fk.x, t);
 #pragma unroll
-        for (int n = 0; n < NSX; ++n) xl[((wave * DK + ks) * NSX + n) * kFragLanes + lane] = t[n];
+        for (int n = 0; n < NSX; ++n) xl[((rt * DK + ks) * NSX + n) * kFragLanes + lane] = t[n];
       } else {
         y[ks].terms(fk.x, kf[ks]);
       }
@@ -96,7 +99,7 @@ __global__ __launch_bounds__(256, DK <= 4 ? 2 : 1) void k_decay_out(DecayArgs a)
     auto features = [&](auto&& rows, const RowFactors& o) {
       project_terms<DK, NSX, NW, false, WHOLE>(weights, rows, acc, lo);
 #pragma unroll
-      for (int e = 0; e < 16; ++e) ph[e] = feature<ELU, WHOLE>(acc[e], WHOLE ? lo[e] : 0.f, o.r, o.c, o.f);
+      for (int e = 0; e < 16; ++e) ph[e] = feature<ELU, WHOLE>(acc[e], WHOLE ? lo[e] : 0.f, o.r, o.c);
       if (part) {
 #pragma unroll
         for (int e = 0; e < 16; ++e)
@@ -106,7 +109,7 @@ __global__ __launch_bounds__(256, DK <= 4 ? 2 : 1) void k_decay_out(DecayArgs a)
     features(
         [&](int ks, uint4(&x)[NSX]) {
           if constexpr (KROWS) {
-            read_terms<NSX>(xl + (wave * DK + ks) * NSX * kFragLanes, x);
+            read_terms<NSX>(xl + (rt * DK + ks) * NSX * kFragLanes, x);
           } else {
 #pragma unroll
             for (int n = 0; n < NSX; ++n) x[n] = kf[ks][n];
@@ -118,7 +121,7 @@ __global__ __launch_bounds__(256, DK <= 4 ? 2 : 1) void k_decay_out(DecayArgs a)
       uint4 t[NT];
       pack_half<NT>(ph, k2, t);
 #pragma unroll
-      for (int s = 0; s < NT; ++s) kl[((wave * 2 + k2) * NT + s) * kFragLanes + lane] = t[s];
+      for (int s = 0; s < NT; ++s) kl[((rt * 2 + k2) * NT + s) * kFragLanes + lane] = t[s];
     }
     features(
         [&](int ks, uint4(&x)[NSX]) {
@@ -148,7 +151,7 @@ __global__ __launch_bounds__(256, DK <= 4 ? 2 : 1) void k_decay_out(DecayArgs a)
     __syncthreads();  // phi(k) of all rows
 #pragma unroll
     for (int jt = 0; jt < 4; ++jt)
-      if (jt <= wave) {
+      if (jt <= rt) {
 #pragma unroll
         for (int k2 = 0; k2 < 2; ++k2) {
           uint4 t[NT];
@@ -166,16 +169,17 @@ __global__ __launch_bounds__(256, DK <= 4 ? 2 : 1) void k_decay_out(DecayArgs a)
     for (int e = 0; e < 16; ++e) Z[ct][e] *= since;
   __syncthreads();
   stage_columns<TX, DT, 4, NT, Values::kClean>(vr, vl, &odd);
+  const TileWeights weights_of(rl, 1);
   __syncthreads();
 #pragma unroll
   for (int jt = 0; jt < 4; ++jt)
-    if (jt <= wave) {
+    if (jt <= rt) {
+      if (jt == rt)
+        weights_of.template apply<true>(S[jt], i, 32 * jt);
+      else
+        weights_of.template apply<false>(S[jt], i, 32 * jt);
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int dist = i - (32 * jt + 8 * (e >> 2) + 4 * lh + (e & 3));
-        S[jt][e] = dist >= 0 ? S[jt][e] * decay(rl, dist) : 0.f;
-        den += S[jt][e];
-      }
+      for (int e = 0; e < 16; ++e) den += S[jt][e];
 #pragma unroll
       for (int k2 = 0; k2 < 2; ++k2) {
         uint4 pf[NP];
@@ -195,7 +199,7 @@ __global__ __launch_bounds__(256, DK <= 4 ? 2 : 1) void k_decay_out(DecayArgs a)
     __syncthreads();
     stage_columns<TX, DT, 4, 1, Values::kMark>(vr, vl, nullptr);
     __syncthreads();
-    for (int jt = 0; jt <= wave; ++jt)
+    for (int jt = 0; jt <= rt; ++jt)
 #pragma unroll
       for (int k2 = 0; k2 < 2; ++k2) {
         floatx16 seen;

@@ -36,7 +36,7 @@ __global__ __launch_bounds__(64 * WAVES, DK <= 4 ? 2 : 1) void k_decay_states(De
   constexpr int NSX = kTermsX<TX>, NW = WHOLE ? 2 : 3, DT = DK / 2, PB = WHOLE || DK == 8 || PATH ? 2 : 4;
   constexpr int BPW = (PB + WAVES - 1) / WAVES;  // blocks of x that a wave stages
   __shared__ __align__(16) uint4 xl[PB * DK * NSX * kFragLanes], vl[PB * DT * 2 * NV * kFragLanes];
-  __shared__ __align__(16) float fr[32 * PB], fc[32 * PB], ff[32 * PB], fd[BACK ? 32 * PB : 4];
+  __shared__ __align__(16) float fr[32 * PB], fc[32 * PB], fd[BACK ? 32 * PB : 4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lr = lane & 31, lh = lane >> 5;
   const int seg = blockIdx.y, bh = blockIdx.x, b = bh / a.H, h = bh % a.H, d = a.d, M = a.M, Mp = a.Mp;
@@ -130,7 +130,7 @@ __global__ __launch_bounds__(64 * WAVES, DK <= 4 ? 2 : 1) void k_decay_states(De
       for (int i = 0; i < BPW; ++i) {
         const int blk = wave + WAVES * i;
         if (blk < PB) {
-          RowFactors o = row_factors<ELU>(row_square<TX, DK>(rx[i]), a.nprf, a.log2_m);
+          RowFactors o = row_factors<ELU, WHOLE>(row_square<TX, DK>(rx[i]), a.nprf, a.log2_m);
 #pragma unroll
           for (int ks = 0; ks < DK; ++ks) {
             uint4 t[NSX];
@@ -141,12 +141,13 @@ __global__ __launch_bounds__(64 * WAVES, DK <= 4 ? 2 : 1) void k_decay_states(De
           if (lh == 0) {
             // the weight of the chunk's end, e^{-rate (cnt - 1 - r)}, goes with the row's factors
             const int r = q0 + 32 * blk + lr;
+            // (elu + 1: as a factor in c's place)
             const float e = -rl * static_cast<float>(BACK ? r : cnt - 1 - r);
             if constexpr (ELU)
-              o.f = r < cnt ? __builtin_amdgcn_exp2f(e) : 0.f;
+              o.c = r < cnt ? __builtin_amdgcn_exp2f(e) : 0.f;
             else
               o.c = r < cnt ? o.c + e : -INFINITY;
-            fr[32 * blk + lr] = o.r, fc[32 * blk + lr] = o.c, ff[32 * blk + lr] = o.f;
+            fr[32 * blk + lr] = o.r, fc[32 * blk + lr] = o.c;
             if constexpr (BACK) fd[32 * blk + lr] = rd[i];
           }
         }
@@ -179,11 +180,12 @@ __global__ __launch_bounds__(64 * WAVES, DK <= 4 ? 2 : 1) void k_decay_states(De
         for (int g = 0; g < 4; ++g) {
           const int at = 32 * blk + 8 * g + 4 * lh;
           const float4 r4 = *reinterpret_cast<const float4*>(fr + at), c4 = *reinterpret_cast<const float4*>(fc + at);
-          float4 f4 = make_float4(1.f, 1.f, 1.f, 1.f);
-          if constexpr (ELU || WHOLE) f4 = *reinterpret_cast<const float4*>(ff + at);
-          const float r_[4] = {r4.x, r4.y, r4.z, r4.w}, c_[4] = {c4.x, c4.y, c4.z, c4.w}, f_[4] = {f4.x, f4.y, f4.z, f4.w};
+          const float r_[4] = {r4.x, r4.y, r4.z, r4.w}, c_[4] = {c4.x, c4.y, c4.z, c4.w};
 #pragma unroll
-          for (int j = 0; j < 4; ++j) ph[4 * g + j] = feature<ELU, WHOLE>(acc[4 * g + j], WHOLE ? lo[4 * g + j] : 0.f, r_[j], c_[j], f_[j]);
+          for (int j = 0; j < 4; ++j) {
+            const float y = feature<ELU, WHOLE>(acc[4 * g + j], WHOLE ? lo[4 * g + j] : 0.f, r_[j], c_[j]);
+            ph[4 * g + j] = ELU ? y * c_[j] : y;
+          }
         }
         if (l >= M) ph = zero16();
         if constexpr (BACK) {

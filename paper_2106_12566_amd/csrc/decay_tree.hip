@@ -36,7 +36,7 @@ __global__ __launch_bounds__(64 * kSplit * RT, sizeof(TX) == 2 && DK <= 4 ? 2 : 
   __shared__ __align__(16) uint4 pl[NP][2][NPP][64];  // P as operands
   __shared__ __align__(16) uint4 vl[RT * DT * 2 * NT * 64];
   __shared__ float dpart[kSplit][32 * RT], dsum[NP][32];
-  __shared__ float fr[2][32 * RT], fc[2][32 * RT], ff[2][32 * RT], fx[2][32 * RT];
+  __shared__ float fr[2][32 * RT], fc[2][32 * RT], fx[2][32 * RT];
   __shared__ unsigned long long seen[32 * RT];
   __shared__ int odd;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -133,9 +133,9 @@ __global__ __launch_bounds__(64 * kSplit * RT, sizeof(TX) == 2 && DK <= 4 ? 2 : 
     fetch_last(f0);
     if (f0 < 32 * kSplit) {  // the first time
       if (stages) {
-        const RowFactors o = row_factors<ELU>(row_square<TX, DK>(raw), a.nprf, a.log2_m);
+        const RowFactors o = row_factors<ELU, WHOLE>(row_square<TX, DK>(raw), a.nprf, a.log2_m);
         const int w = wave & 1, t = wave >> 1;
-        if (lh == 0) fr[w][32 * t + lr] = o.r, fc[w][32 * t + lr] = o.c, ff[w][32 * t + lr] = o.f, fx[w][32 * t + lr] = o.x;
+        if (lh == 0) fr[w][32 * t + lr] = o.r, fc[w][32 * t + lr] = o.c, fx[w][32 * t + lr] = o.x;
 #pragma unroll
         for (int ks = 0; ks < DK; ++ks)
 #pragma unroll
@@ -162,10 +162,10 @@ __global__ __launch_bounds__(64 * kSplit * RT, sizeof(TX) == 2 && DK <= 4 ? 2 : 
             x.terms(scale, y);
           },
           acc, lo);
-      const float r_ = fr[w][32 * t + lr], c_ = fc[w][32 * t + lr], f_ = ff[w][32 * t + lr];
+      const float r_ = fr[w][32 * t + lr], c_ = fc[w][32 * t + lr];
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
-        ph[e] = feature<ELU, WHOLE>(acc[e], WHOLE ? lo[e] : 0.f, r_, c_, f_);
+        ph[e] = feature<ELU, WHOLE>(acc[e], WHOLE ? lo[e] : 0.f, r_, c_);
         if (f0 + 8 * (e >> 2) + 4 * lh + (e & 3) >= M) ph[e] = 0.f;
       }
       pack_half<NT>(ph, 0, p[0]);
