@@ -22,22 +22,34 @@ namespace krpe {
 
 // 128 rows as operands over their columns: f[tile][ks][term][64], lane: row, column
 // 16 ks + 8 (t / 4) + 4 lh + t % 4; zeros past the array's end and past d.
-template <typename T, int DK, int NT>
-__device__ __forceinline__ void stage_rows(const Rows<T>& x, uint4* __restrict__ f) {
+template <typename T, int DK>
+struct RowTile {
+  Raw4<T> u[DK][2];
+  __device__ __forceinline__ void fetch(const Rows<T>& x) {
 #pragma unroll
-  for (int n = 0; n < DK; ++n) {
-    const int e = threadIdx.x + 256 * n, half = e & 1, ks = (e >> 1) % DK, r = e / (2 * DK);
-    float u[4], w[4];
-    load4(x, x.at(r), 16 * ks + 4 * half, u);
-    load4(x, x.at(r), 16 * ks + 4 * half + 8, w);
-    uint32_t p[4][NT];
-    split_pair<NT>(u[0], u[1], p[0]), split_pair<NT>(u[2], u[3], p[1]);
-    split_pair<NT>(w[0], w[1], p[2]), split_pair<NT>(w[2], w[3], p[3]);
-#pragma unroll
-    for (int s = 0; s < NT; ++s)
-      f[(((r >> 5) * DK + ks) * NT + s) * kFragLanes + 32 * half + (r & 31)] = make_uint4(p[0][s], p[1][s], p[2][s], p[3][s]);
+    for (int n = 0; n < DK; ++n) {
+      const int e = threadIdx.x + 256 * n, half = e & 1, ks = (e >> 1) % DK, r = e / (2 * DK);
+      u[n][0].load(x, x.at(r), 16 * ks + 4 * half);
+      u[n][1].load(x, x.at(r), 16 * ks + 4 * half + 8);
+    }
   }
-}
+  template <int NT>
+  __device__ __forceinline__ void put(uint4* __restrict__ f) const {
+#pragma unroll
+    for (int n = 0; n < DK; ++n) {
+      const int e = threadIdx.x + 256 * n, half = e & 1, ks = (e >> 1) % DK, r = e / (2 * DK);
+      float v[4], w[4];
+      u[n][0].values(v);
+      u[n][1].values(w);
+      uint32_t p[4][NT];
+      split_pair<NT>(v[0], v[1], p[0]), split_pair<NT>(v[2], v[3], p[1]);
+      split_pair<NT>(w[0], w[1], p[2]), split_pair<NT>(w[2], w[3], p[3]);
+#pragma unroll
+      for (int s = 0; s < NT; ++s)
+        f[(((r >> 5) * DK + ks) * NT + s) * kFragLanes + 32 * half + (r & 31)] = make_uint4(p[0][s], p[1][s], p[2][s], p[3][s]);
+    }
+  }
+};
 
 // 32 rows of W from f0 turned: operands tl[ct][k2][term][64], lane: dimension, features in the
 // slots (elu + 1: the identity).
@@ -120,18 +132,37 @@ __device__ __forceinline__ void store_row_gradient(const Rows<TX>& x, uint32_t a
     }
 }
 
+// Terms of the other rows' values: v, exact in one where it is bf16, or g.
+template <typename TX, int NT, int SIDE>
+constexpr int kValueTerms = sizeof(TX) == 2 && SIDE == 0 ? 1 : NT;
+// LDS in fragments: what the two passes and the step between work on; then the values' columns, there
+// from the start, and after these R.  Where that is too much the columns come after the first pass,
+// in its place.
+template <typename TX, int DK, int NT, int SIDE>
+struct GradSizes {
+  static constexpr int NV = kValueTerms<TX, NT, SIDE>;
+  static constexpr int kLoop = DK * 2 + 8 * NT + DK * NT + DK * NT, kRows = 4 * DK * NV;
+  static constexpr int kWork = kLoop > kRows ? kLoop : kRows;
+  static constexpr int kColumns = 4 * DK * NV, kR = 12 * NT;
+  static constexpr bool kEarly = kWork + kColumns <= 152;
+  static constexpr int kAll = kWork + (kEarly && kColumns > kR ? kColumns : kR);
+};
+
 template <typename TX, int DK, int NT, int SIDE, bool ELU>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k_decay_grad(DecayArgs a) {
+__global__ __launch_bounds__(256, sizeof(TX) == 2 && DK <= 4 ? 2 : 1) void k_decay_grad(DecayArgs a) {
   using TG = typename std::conditional<SIDE == 0, TX, float>::type;  // values of the other rows: v, or g
   constexpr bool WHOLE = sizeof(TX) == 4;
-  constexpr int NSX = kTermsX<TX>, DT = DK / 2, NW = WHOLE ? 2 : 3;
+  constexpr int NSX = kTermsX<TX>, DT = DK / 2, NW = 2;
   extern __shared__ __align__(16) uint4 smem[];
-  // first pass                                        second pass
-  uint4* const wl = smem;                           // wl   [DK][NW][64]
-  uint4* const kl = wl + DK * NW * kFragLanes;      // kl   [4][2][NT][64]
-  uint4* const sl = kl + 8 * NT * kFragLanes;       // sl   [DT][2][NT][64]; then [DK][NT][64]
-  uint4* const tl = sl + DK * NT * kFragLanes;      // tl   [DT][2][NT][64]
-  uint4* const vl = smem;                           // between: columns [4][DT][2][NT][64], rows [4][DK][NT][64]
+  constexpr int NV = kValueTerms<TX, NT, SIDE>, NG = kValueTerms<TX, NT, 1 - SIDE>;
+  uint4* const wl = smem;                           // W [DK][NW][64]
+  uint4* const kl = wl + DK * NW * kFragLanes;      // features of the other rows [4][2][NT][64]
+  uint4* const sl = kl + 8 * NT * kFragLanes;       // the state [DT][2][NT][64], second pass [DK][NT][64]
+  uint4* const tl = sl + DK * NT * kFragLanes;      // second pass: W turned [DT][2][NT][64]
+  uint4* const vl = smem;                           // between: the values' rows [4][DK][NV][64]
+  using Sizes = GradSizes<TX, DK, NT, SIDE>;
+  uint4* const rl_ = smem + Sizes::kWork * kFragLanes;  // R off the diagonal [6][2][NT][64]
+  uint4* const cl = Sizes::kEarly ? rl_ : smem;         // the values' columns [4][DT][2][NV][64]
   __shared__ __align__(16) float sden[32], sgd[kChunk];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lr = lane & 31, lh = lane >> 5;
@@ -165,12 +196,16 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k
       weights_of.template apply<false>(x, i, 32 * t);
   };
   WeightTile<DK, NW, ELU, WHOLE> wt;
+  wt.fetch(W, 0);
+  StateTile<DT, NT, false> state(old, pre, wold, d, a.Mp);
+  state.fetch(0);
   uint4 of[DK][NSX], tf[DK][NSX];
   RowFactors fo, ft;
   {
     Raw8<TX> x[DK], y[DK];
     fetch_row<TX, DK>(own, own.at(i), x);
     fetch_row<TX, DK>(oth, oth.at(i), y);
+    if constexpr (Sizes::kEarly) stage_columns<TG, DT, 4, NV, Values::kAsIs>(vals, cl, nullptr);
     fo = row_factors<ELU, WHOLE>(row_square<TX, DK>(x), a.nprf, a.log2_m);
     ft = row_factors<ELU, WHOLE>(row_square<TX, DK>(y), a.nprf, a.log2_m);
 #pragma unroll
@@ -188,6 +223,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k
   // [g | gd] of the lane's row (SIDE 0), or its values (SIDE 1)
   floatx16 G[DT];
   float gd = 1.f;
+  RowTile<TG, DK> vrows;
   {
     floatx16 S[4], Z[DT];
 #pragma unroll
@@ -195,9 +231,6 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k
 #pragma unroll
     for (int t = 0; t < DT; ++t) Z[t] = zero16();
     float den = 0.f;
-    StateTile<DT, NT, false> state(old, pre, wold, d, a.Mp);
-    wt.fetch(W, 0);
-    state.fetch(0);
 #pragma unroll 1
     for (int f0 = 0; f0 < a.Mp; f0 += 32) {
       // (the waves have all read the operands before: they have passed the barrier after phi)
@@ -258,16 +291,26 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k
           }
         }
     }
+    if constexpr (!Sizes::kEarly) {
+      __syncthreads();
+      stage_columns<TG, DT, 4, NV, Values::kAsIs>(vals, cl, nullptr);
+      __syncthreads();
+    }
+    // (the next step's operands are asked for here)
+    vrows.fetch(vals);
+    const Rows<TX> mine(static_cast<const TX*>(SIDE == 0 ? a.dz : a.v) + from, cnt, d);
+    Raw4<TX> m4[DT][4];
+#pragma unroll
+    for (int ct = 0; ct < DT; ++ct)
+#pragma unroll
+      for (int g4 = 0; g4 < 4; ++g4) m4[ct][g4].load(mine, mine.at(i), 32 * ct + 8 * g4 + 4 * lh);
+    if (SIDE == 1 && threadIdx.x < kChunk)
+      sgd[threadIdx.x] = static_cast<int>(threadIdx.x) < cnt ? a.gd[static_cast<size_t>(bh) * a.n + p0 + threadIdx.x] : 0.f;
     den *= share;
 #pragma unroll
     for (int ct = 0; ct < DT; ++ct)
 #pragma unroll
       for (int e = 0; e < 16; ++e) Z[ct][e] *= share;
-    __syncthreads();
-    stage_columns<TG, DT, 4, NT, Values::kAsIs>(vals, vl, nullptr);
-    if (SIDE == 1 && threadIdx.x < kChunk)
-      sgd[threadIdx.x] = static_cast<int>(threadIdx.x) < cnt ? a.gd[static_cast<size_t>(bh) * a.n + p0 + threadIdx.x] : 0.f;
-    __syncthreads();
 #pragma unroll
     for (int t = 0; t < 4; ++t)
       if (uses(t)) {
@@ -282,16 +325,15 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k
           pack_half<NT>(S[t], k2, pf);
 #pragma unroll
           for (int ct = 0; ct < DT; ++ct) {
-            uint4 f[NT];
-            read_terms<NT>(vl + ((t * DT + ct) * 2 + k2) * NT * kFragLanes, f);
-            Z[ct] = mfma_terms<NT, NT>(f, pf, Z[ct]);
+            uint4 f[NV];
+            read_terms<NV>(cl + ((t * DT + ct) * 2 + k2) * NV * kFragLanes, f);
+            Z[ct] = mfma_terms<NV, NT>(f, pf, Z[ct]);
           }
         }
       }
     if constexpr (SIDE == 0) {
       den += __shfl_xor(den, 32);
       const float inv = i < cnt ? 1.f / den : 0.f;
-      const Rows<TX> dz(static_cast<const TX*>(a.dz) + from, cnt, d);
       float* __restrict__ g = a.g + from + static_cast<size_t>(i) * d;
       float dot = 0.f;
 #pragma unroll
@@ -300,7 +342,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k
         for (int g4 = 0; g4 < 4; ++g4) {
           const int c = 32 * ct + 8 * g4 + 4 * lh;
           float u[4];
-          load4(dz, dz.at(i), c, u);
+          m4[ct][g4].values(u);
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             u[j] *= inv;
@@ -312,7 +354,6 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k
       gd = -(dot + __shfl_xor(dot, 32)) * inv;
       if (i < cnt && lh == 0) a.gd[static_cast<size_t>(bh) * a.n + p0 + i] = gd;
     } else {
-      const Rows<TX> v(static_cast<const TX*>(a.v) + from, cnt, d);
       TX* __restrict__ dv = static_cast<TX*>(a.dv) + from + static_cast<size_t>(i) * d;
 #pragma unroll
       for (int ct = 0; ct < DT; ++ct)
@@ -320,7 +361,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k
         for (int g4 = 0; g4 < 4; ++g4) {
           const int c = 32 * ct + 8 * g4 + 4 * lh;
           float u[4];
-          load4(v, v.at(i), c, u);
+          m4[ct][g4].values(u);
 #pragma unroll
           for (int j = 0; j < 4; ++j) G[ct][4 * g4 + j] = u[j];
           const float o[4] = {Z[ct][4 * g4], Z[ct][4 * g4 + 1], Z[ct][4 * g4 + 2], Z[ct][4 * g4 + 3]};
@@ -330,23 +371,26 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k
   }
   // R = e^{-rate (i - j)} (G_i . [v_j | 1]) as operands, and the lane's own values with the
   // weight of the state outside the chunk
-  uint4 R[4][2][NT], gf[DT][2][NT];
+  // (R of the diagonal tile stays in registers, of the others in LDS: each wave reads its own)
+  uint4 R[2][NT], gf[DT][2][NT];
+  auto r_at = [&](int t) { return rl_ + (SIDE == 0 ? rt * (rt - 1) / 2 + t : (3 - rt) * (2 - rt) / 2 + t - rt - 1) * 2 * NT * kFragLanes; };
+  __syncthreads();  // the first pass's operands and the columns are consumed
+  vrows.template put<NV>(vl);
   __syncthreads();
-  stage_rows<TG, DK, NT>(vals, vl);
-  __syncthreads();
+  uint4 ge[DT][2][NG];
 #pragma unroll
   for (int ct = 0; ct < DT; ++ct)
 #pragma unroll
-    for (int k2 = 0; k2 < 2; ++k2) pack_half<NT>(G[ct], k2, gf[ct][k2]);
+    for (int k2 = 0; k2 < 2; ++k2) pack_half<NG>(G[ct], k2, ge[ct][k2]);
 #pragma unroll
   for (int t = 0; t < 4; ++t)
     if (uses(t)) {
       floatx16 r = zero16();
 #pragma unroll
       for (int ks = 0; ks < DK; ++ks) {
-        uint4 f[NT];
-        read_terms<NT>(vl + (t * DK + ks) * NT * kFragLanes, f);
-        r = mfma_terms<NT, NT>(f, gf[ks >> 1][ks & 1], r);
+        uint4 f[NV];
+        read_terms<NV>(vl + (t * DK + ks) * NV * kFragLanes, f);
+        r = mfma_terms<NV, NG>(f, ge[ks >> 1][ks & 1], r);
       }
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
@@ -354,8 +398,18 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k
         r[e] += one;
       }
       weigh(r, t);
-      pack_half<NT>(r, 0, R[t][0]);
-      pack_half<NT>(r, 1, R[t][1]);
+      if (t == rt) {
+        pack_half<NT>(r, 0, R[0]);
+        pack_half<NT>(r, 1, R[1]);
+      } else {
+#pragma unroll
+        for (int k2 = 0; k2 < 2; ++k2) {
+          uint4 f[NT];
+          pack_half<NT>(r, k2, f);
+#pragma unroll
+          for (int s = 0; s < NT; ++s) r_at(t)[(k2 * NT + s) * kFragLanes + lane] = f[s];
+        }
+      }
     }
 #pragma unroll
   for (int ct = 0; ct < DT; ++ct) {
@@ -370,20 +424,20 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k
   for (int t = 0; t < DT; ++t) Y[t] = zero16();
   float psum = 0.f;
   // the state with rows l and the columns in the slots, and W with rows c and features in them
-  StateTile<DT, NT, true> state(old, pre, wold, d, a.Mp);
+  StateTile<DT, NT, true> turned(old, pre, wold, d, a.Mp);
   TurnedTile<DT, NT, ELU> tt;
   wt.fetch(W, 0);
-  state.fetch(0);
+  turned.fetch(0);
   tt.fetch(W, 0);
 #pragma unroll 1
   for (int f0 = 0; f0 < a.Mp; f0 += 32) {
     __syncthreads();  // the operands before consumed
     wt.put(wl);
-    if (state.any()) state.put(sl, sden);
+    if (turned.any()) turned.put(sl, sden);
     tt.put(tl);
     if (f0 + 32 < a.Mp) {
       wt.fetch(W, f0 + 32);
-      state.fetch(f0 + 32);
+      turned.fetch(f0 + 32);
       tt.fetch(W, f0 + 32);
     }
     __syncthreads();
@@ -403,7 +457,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k
 #pragma unroll
       for (int s = 0; s < NT; ++s) kl[((rt * 2 + k2) * NT + s) * kFragLanes + lane] = t[s];
     }
-    if (state.any()) {
+    if (turned.any()) {
 #pragma unroll
       for (int ks = 0; ks < DK; ++ks) {
         uint4 f[NT];
@@ -427,9 +481,15 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1))) void k
       if (uses(t)) {
 #pragma unroll
         for (int k2 = 0; k2 < 2; ++k2) {
-          uint4 f[NT];
+          uint4 f[NT], y[NT];
           read_terms<NT>(kl + (t * 2 + k2) * NT * kFragLanes, f);
-          df = mfma_terms<NT, NT>(f, R[t][k2], df);
+          if (t == rt) {
+#pragma unroll
+            for (int s = 0; s < NT; ++s) y[s] = R[k2][s];
+          } else {
+            read_terms<NT>(r_at(t) + k2 * NT * kFragLanes, y);
+          }
+          df = mfma_terms<NT, NT>(f, y, df);
         }
       }
 #pragma unroll
@@ -455,21 +515,20 @@ namespace {
 
 template <typename TX, int DK, bool ELU>
 hipError_t go(const DecayArgs& a, hipStream_t st) {
-  constexpr int NT = sizeof(TX) == 2 ? 2 : 3, NV = sizeof(TX) == 2 ? 1 : 3, DT = DK / 2;
-  constexpr int loop = DK * (sizeof(TX) == 2 ? 3 : 2) + 8 * NT + DK * NT + DT * 2 * NT, mid = 4 * DK * NT;
-  constexpr int lds = (loop > mid ? loop : mid) * 1024;
-  if constexpr (lds > 65536) {
+  constexpr int NT = sizeof(TX) == 2 ? 2 : 3, NV = sizeof(TX) == 2 ? 1 : 3;
+  constexpr int lds0 = GradSizes<TX, DK, NT, 0>::kAll * 1024, lds1 = GradSizes<TX, DK, NT, 1>::kAll * 1024;
+  if constexpr (lds0 > 65536)
     (void)hipFuncSetAttribute(reinterpret_cast<const void*>(&k_decay_grad<TX, DK, NT, 0, ELU>),
-                              hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+                              hipFuncAttributeMaxDynamicSharedMemorySize, lds0);
+  if constexpr (lds1 > 65536)
     (void)hipFuncSetAttribute(reinterpret_cast<const void*>(&k_decay_grad<TX, DK, NT, 1, ELU>),
-                              hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-  }
+                              hipFuncAttributeMaxDynamicSharedMemorySize, lds1);
   const dim3 grid(static_cast<unsigned>(a.B) * a.H * a.nchunk), block(256);
   const bool sums = a.nchunk > 1;  // (a single chunk has no state outside it)
   if (sums) launch_decay_states<TX, TX, DK, NT, NV, ELU, Sums::kForth>(a, st);
-  hipLaunchKernelGGL((k_decay_grad<TX, DK, NT, 0, ELU>), grid, block, lds, st, a);
+  hipLaunchKernelGGL((k_decay_grad<TX, DK, NT, 0, ELU>), grid, block, lds0, st, a);
   if (sums) launch_decay_states<TX, float, DK, NT, NT, ELU, Sums::kBack>(a, st);
-  hipLaunchKernelGGL((k_decay_grad<TX, DK, NT, 1, ELU>), grid, block, lds, st, a);
+  hipLaunchKernelGGL((k_decay_grad<TX, DK, NT, 1, ELU>), grid, block, lds1, st, a);
   return hipGetLastError();
 }
 template <typename TX, bool ELU>

@@ -26,7 +26,9 @@ __global__ __launch_bounds__(256, DK <= 4 ? 2 : 1) void k_decay_out(DecayArgs a)
   uint4* const sl = wl + DK * NW * kFragLanes;       // [DT][2][NP][64]
   uint4* const kl = sl + DT * 2 * NP * kFragLanes;   // [4][2][NT][64]
   uint4* const xl = kl + 8 * NT * kFragLanes;        // KROWS: k [4][DK][NSX][64], each wave its own
-  uint4* const vl = smem;                            // [4][DT][2][NT][64], after the features
+  // the values' columns [4][DT][2][NT][64]: from the start, or after the features in their place
+  constexpr bool EARLY = !WHOLE;
+  uint4* const vl = EARLY ? kl + 8 * NT * kFragLanes : smem;
   __shared__ __align__(16) float sden[32];
   __shared__ int odd;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -61,6 +63,13 @@ __global__ __launch_bounds__(256, DK <= 4 ? 2 : 1) void k_decay_out(DecayArgs a)
     Raw8<TX> x[DK], y[DK];
     fetch_row<TX, DK>(qr, qr.at(i), x);
     fetch_row<TX, DK>(kr, kr.at(i), y);
+    if constexpr (EARLY) {
+      if (threadIdx.x == 0) odd = 0;
+      ColumnTile<TX, DT, 4, 256> t;
+      t.fetch(vr, [&](int r) { return vr.at(r); });
+      __syncthreads();  // (odd is clear)
+      t.template put<NT, Values::kClean>(vl, &odd);
+    }
     fq = row_factors<ELU, WHOLE>(row_square<TX, DK>(x), a.nprf, a.log2_m);
     fk = row_factors<ELU, WHOLE>(row_square<TX, DK>(y), a.nprf, a.log2_m);
 #pragma unroll
@@ -82,7 +91,7 @@ __global__ __launch_bounds__(256, DK <= 4 ? 2 : 1) void k_decay_out(DecayArgs a)
 #pragma unroll
   for (int t = 0; t < DT; ++t) Z[t] = zero16();
   float den = 0.f;
-  if (threadIdx.x == 0) odd = 0;
+  if (!EARLY && threadIdx.x == 0) odd = 0;
   auto weights = [&](int ks, uint4(&w)[NW]) { read_terms<NW>(wl + ks * NW * kFragLanes, w); };
 #pragma unroll 1
   for (int f0 = 0; f0 < a.Mp; f0 += 32) {
@@ -167,10 +176,12 @@ __global__ __launch_bounds__(256, DK <= 4 ? 2 : 1) void k_decay_out(DecayArgs a)
   for (int ct = 0; ct < DT; ++ct)
 #pragma unroll
     for (int e = 0; e < 16; ++e) Z[ct][e] *= since;
-  __syncthreads();
-  stage_columns<TX, DT, 4, NT, Values::kClean>(vr, vl, &odd);
+  if constexpr (!EARLY) {
+    __syncthreads();
+    stage_columns<TX, DT, 4, NT, Values::kClean>(vr, vl, &odd);
+  }
   const TileWeights weights_of(rl, 1);
-  __syncthreads();
+  if constexpr (!EARLY) __syncthreads();
 #pragma unroll
   for (int jt = 0; jt < 4; ++jt)
     if (jt <= rt) {
@@ -241,7 +252,7 @@ hipError_t go(const DecayArgs& a, hipStream_t st) {
   if (a.nchunk > 0) {
     constexpr int NSX = kTermsX<TX>, NW = 2;
     constexpr int feat = DK * NW + DT * 2 * NP + 8 * NT + (sizeof(TX) == 4 ? 4 * DK * NSX : 0), vals = 8 * DT * NT;
-    constexpr int lds = (feat > vals ? feat : vals) * 1024;
+    constexpr int lds = (sizeof(TX) == 2 ? feat + vals : feat > vals ? feat : vals) * 1024;
     if constexpr (lds > 65536)
       (void)hipFuncSetAttribute(reinterpret_cast<const void*>(&k_decay_out<TX, DK, NT, NP, ELU>),
                                 hipFuncAttributeMaxDynamicSharedMemorySize, lds);
