@@ -61,33 +61,32 @@ __device__ __forceinline__ float decay(float rl, int dist) { return __builtin_am
 
 // The weights e^{-rate dist} of a 32 x 32 result's rows: dist = sign (i - j) for the lane's row i and rows
 // j = base + 8 (e / 4) + 4 lh + e % 4 along the registers; zero below 0 (EDGE: where that can be).
-// Where 32 positions keep 2^-60, as the product of the lane's weight and 16 others that all tiles share.
+// As products of a weight for each four rows and one of four that all share, which a rate of 40 bits
+// a position keeps in range; beyond, where the next position weighs less than 2^-40, only dist 0 counts.
 struct TileWeights {
   float rl;
-  bool near;  // uniform
-  float t[16];
   int sign;
-  __device__ __forceinline__ TileWeights(float rl_, int sign_) : rl(rl_), near(fabsf(rl_) * 32.f < 60.f), sign(sign_) {
-    const int lh = (threadIdx.x & 63) >> 5;
+  bool self;  // uniform
+  float t[4];
+  __device__ __forceinline__ TileWeights(float rl_, int sign_) : rl(rl_ > 40.f ? 40.f : rl_), sign(sign_), self(rl_ > 40.f) {
 #pragma unroll
-    for (int e = 0; e < 16; ++e) t[e] = decay(rl, -sign * (8 * (e >> 2) + 4 * lh + (e & 3)));
+    for (int j = 0; j < 4; ++j) t[j] = decay(rl, -sign * j);
   }
   template <bool EDGE>
   __device__ __forceinline__ void apply(floatx16& x, int i, int base) const {
-    const int lh = (threadIdx.x & 63) >> 5;
-    const int d0 = sign * (i - base);
-    if (near) {
-      const float w = decay(rl, d0);
+    const int d0 = sign * (i - base - 4 * static_cast<int>((threadIdx.x & 63) >> 5));
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const float y = x[e] * (w * t[e]);
-        x[e] = !EDGE || d0 - sign * (8 * (e >> 2) + 4 * lh + (e & 3)) >= 0 ? y : 0.f;
-      }
-    } else {
+    for (int g = 0; g < 4; ++g) {
+      const float w = self ? 0.f : decay(rl, d0 - sign * 8 * g);
 #pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const int dist = d0 - sign * (8 * (e >> 2) + 4 * lh + (e & 3));
-        x[e] = dist >= 0 ? x[e] * decay(rl, dist) : 0.f;
+      for (int j = 0; j < 4; ++j) {
+        const float y = x[4 * g + j] * (w * t[j]);
+        if constexpr (EDGE) {
+          const int dist = d0 - sign * (8 * g + j);
+          x[4 * g + j] = dist > 0 ? y : (dist == 0 ? x[4 * g + j] : 0.f);
+        } else {
+          x[4 * g + j] = y;
+        }
       }
     }
   }

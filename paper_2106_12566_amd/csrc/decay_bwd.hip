@@ -163,7 +163,7 @@ __global__ __launch_bounds__(256, sizeof(TX) == 2 && DK <= 4 ? 2 : 1) void k_dec
   using Sizes = GradSizes<TX, DK, NT, SIDE>;
   uint4* const rl_ = smem + Sizes::kWork * kFragLanes;  // R off the diagonal [6][2][NT][64]
   uint4* const cl = Sizes::kEarly ? rl_ : smem;         // the values' columns [4][DT][2][NV][64]
-  __shared__ __align__(16) float sden[32], sgd[kChunk];
+  __shared__ __align__(16) float sden[32], sgd[kChunk], fr[kChunk], fc[kChunk];  // fr, fc: the other rows' factors
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lr = lane & 31, lh = lane >> 5;
   const int ch = blockIdx.x % a.nchunk, bh = blockIdx.x / a.nchunk, b = bh / a.H, h = bh % a.H, d = a.d;
@@ -210,6 +210,7 @@ __global__ __launch_bounds__(256, sizeof(TX) == 2 && DK <= 4 ? 2 : 1) void k_dec
     ft = row_factors<ELU, WHOLE>(row_square<TX, DK>(y), a.nprf, a.log2_m);
 #pragma unroll
     for (int ks = 0; ks < DK; ++ks) x[ks].terms(fo.x, of[ks]), y[ks].terms(ft.x, tf[ks]);
+    if (lh == 0) fr[i] = ft.r, fc[i] = ft.c;
   }
   auto own_rows = [&](int ks, uint4(&x)[NSX]) {
 #pragma unroll
@@ -442,12 +443,15 @@ __global__ __launch_bounds__(256, sizeof(TX) == 2 && DK <= 4 ? 2 : 1) void k_dec
     }
     __syncthreads();
     floatx16 acc, lo, ph, df = zero16();
-    // features of the other rows with the positions along the registers: their factors by lane
+    // features of the other rows, the positions along the registers
     project_terms<DK, NSX, NW, true, WHOLE>(weights, other_rows, acc, lo);
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const int from = 8 * (e >> 2) + 4 * lh + (e & 3);  // the lane that holds this row's factors
-      ph[e] = feature<ELU, WHOLE>(acc[e], WHOLE ? lo[e] : 0.f, __shfl(ft.r, from), __shfl(ft.c, from));
+    for (int g = 0; g < 4; ++g) {
+      const float4 r4 = *reinterpret_cast<const float4*>(fr + 32 * rt + 8 * g + 4 * lh);
+      const float4 c4 = *reinterpret_cast<const float4*>(fc + 32 * rt + 8 * g + 4 * lh);
+      const float r_[4] = {r4.x, r4.y, r4.z, r4.w}, c_[4] = {c4.x, c4.y, c4.z, c4.w};
+#pragma unroll
+      for (int j = 0; j < 4; ++j) ph[4 * g + j] = feature<ELU, WHOLE>(acc[4 * g + j], WHOLE ? lo[4 * g + j] : 0.f, r_[j], c_[j]);
     }
     if (f0 + lr >= a.M) ph = zero16();
 #pragma unroll
