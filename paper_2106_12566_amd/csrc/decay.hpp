@@ -216,10 +216,10 @@ __device__ __forceinline__ void fetch_row(const Rows<TX>& rows, uint32_t o, Raw8
 #pragma unroll
   for (int ks = 0; ks < DK; ++ks) x[ks].load(rows, o, 16 * ks + 8 * lh);
 }
-// Its squared norm, in eight partial sums a lane (off by a few 2^-25 of itself: at the sizes where
-// features stay in range that is less than the rounding of the exponent).
+// Its squared norm (it is the same for every feature: an error of it weighs on the whole position), in
+// sixteen partial sums added in fp64.
 template <typename TX, int DK>
-__device__ __forceinline__ float row_square(const Raw8<TX> (&x)[DK]) {
+__device__ __forceinline__ double row_square(const Raw8<TX> (&x)[DK]) {
   float p[8] = {};
 #pragma unroll
   for (int ks = 0; ks < DK; ++ks) {
@@ -228,23 +228,28 @@ __device__ __forceinline__ float row_square(const Raw8<TX> (&x)[DK]) {
 #pragma unroll
     for (int t = 0; t < 8; ++t) p[t] = fmaf(v[t], v[t], p[t]);
   }
-  const float s = ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+  double s = p[0];
+#pragma unroll
+  for (int t = 1; t < 8; ++t) s += static_cast<double>(p[t]);
   return s + __shfl_xor(s, 32);
 }
 
 // What phi takes of a row: PRF 2^(s r + c) of the projection s, r = log2(e) (over ||x|| when
-// normalising), c = -||x||^2 / 2 log2(e) - log2(sqrt(m)); elu + 1 r alone.  x: what the operand's
-// terms were scaled by (fp32 rows: a power of two that brings them below 1, which r makes good).
+// normalising), c = -||x||^2 / 2 log2(e) - log2(sqrt(m)); elu + 1 r alone.  f: what the rounding of c
+// left, as a part of s (of its accumulator lo; for the states, it weighs little on a ratio).  x: what the operand's terms were scaled by (fp32
+// rows: a power of two that brings them below 1, which r makes good).
 struct RowFactors {
-  float r, c, x;
+  float r, c, f, x;
 };
 template <bool ELU, bool WHOLE>
-__device__ __forceinline__ RowFactors row_factors(float sq, bool nprf, double log2_m) {
-  const bool nz = sq > 0.f;
-  const float norm = sqrtf(sq);
+__device__ __forceinline__ RowFactors row_factors(double sq, bool nprf, double log2_m) {
+  const bool nz = sq > 0.0;
+  const float norm = sqrtf(static_cast<float>(sq));
   RowFactors o;
   o.r = (ELU ? 1.f : static_cast<float>(kLog2e)) * (nprf ? (nz ? 1.f / norm : 0.f) : 1.f);
-  o.c = static_cast<float>(log2_m) - (nprf ? (nz ? 0.5f : 0.f) : 0.5f * sq) * static_cast<float>(kLog2e);
+  const double c = log2_m - (nprf ? (nz ? 0.5 : 0.0) : 0.5 * sq) * kLog2e;
+  o.c = static_cast<float>(c);
+  o.f = 0.f;
   o.x = 1.f;
   if constexpr (WHOLE) {
     const unsigned n = __float_as_uint(norm) >> 23;  // |x| < 2^(n - 126)
@@ -252,6 +257,7 @@ __device__ __forceinline__ RowFactors row_factors(float sq, bool nprf, double lo
     o.x = __uint_as_float((253u - e) << 23);
     o.r *= __uint_as_float((e + 1u) << 23);
   }
+  if (!ELU && nz && isfinite(o.c)) o.f = static_cast<float>(c - static_cast<double>(o.c)) / o.r * (WHOLE ? kLoScale : 1.f);
   return o;
 }
 // WHOLE: the projection in two accumulators, lo in units of 2^-11 (fp32 rows).
@@ -299,13 +305,13 @@ __device__ __forceinline__ void weight_terms(const float (&v)[8], uint4 (&t)[NW]
 }
 template <int DK, int NW, bool ELU, bool WHOLE>
 struct WeightTile {
-  static constexpr int N = 32 * 2 * DK / 256 > 0 ? 32 * 2 * DK / 256 : 1;
+  static constexpr int N = (64 * DK + 255) / 256;
   float v[N][8];
   __device__ __forceinline__ void fetch(const Rows<float>& W, int f0) {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int e = threadIdx.x + 256 * i;
-      if (DK * 64 < 256 && e >= 64 * DK) return;
+      if (N * 256 > 64 * DK && e >= 64 * DK) return;
       load_weights<ELU>(W, f0 + e / (2 * DK), 8 * (e % (2 * DK)), v[i]);
     }
   }
@@ -313,7 +319,7 @@ struct WeightTile {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
       const int e = threadIdx.x + 256 * i, fl = e / (2 * DK), c = e % (2 * DK);
-      if (DK * 64 < 256 && fl >= 32) return;
+      if (N * 256 > 64 * DK && fl >= 32) return;
       uint4 t[NW];
       weight_terms<NW, WHOLE>(v[i], t);
       uint4* __restrict__ o = wf + (c >> 1) * NW * kFragLanes + (c & 1) * 32 + fl;
@@ -324,11 +330,12 @@ struct WeightTile {
 };
 
 // Projections of 32 rows on 32 features: with WHOLE h h (acc) and h l + l h (lo, in units of 2^-11)
-// apart, else all products of bf16 terms in one sum, the small ones first.
+// apart; products of bf16 terms in one sum, the small ones first, or with three terms of W the first
+// one's (acc) apart from the others (lo), so that the large sum takes few roundings.  lo comes with
+// what it begins with (the rows' f).
 template <int DK, int NSX, int NW, bool XROWS, bool WHOLE, typename FW, typename FX>
 __device__ __forceinline__ void project_terms(FW&& weights, FX&& rows, floatx16& acc, floatx16& lo) {
   acc = zero16();
-  if constexpr (WHOLE) lo = zero16();
   auto mul = [](uint4 w, uint4 x, floatx16 c) {
     if constexpr (WHOLE)
       return XROWS ? mfma_f16(x, w, c) : mfma_f16(w, x, c);
@@ -345,7 +352,12 @@ __device__ __forceinline__ void project_terms(FW&& weights, FX&& rows, floatx16&
       lo = mul(w[1], x[0], lo);
     } else {
 #pragma unroll
-      for (int s = NW - 1; s >= 1; --s) acc = mul(w[s], x[0], acc);
+      for (int s = NW - 1; s >= 1; --s) {
+        if constexpr (NW == 3)
+          lo = mul(w[s], x[0], lo);
+        else
+          acc = mul(w[s], x[0], acc);
+      }
     }
     acc = mul(w[0], x[0], acc);
   }

@@ -244,6 +244,7 @@ __global__ __launch_bounds__(256, sizeof(TX) == 2 && DK <= 4 ? 2 : 1) void k_dec
       __syncthreads();
       floatx16 acc, lo, ph;
       const bool part = f0 + 32 > a.M;
+      lo = zero16();
       project_terms<DK, NSX, NW, false, WHOLE>(weights, other_rows, acc, lo);
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
@@ -257,6 +258,7 @@ __global__ __launch_bounds__(256, sizeof(TX) == 2 && DK <= 4 ? 2 : 1) void k_dec
 #pragma unroll
         for (int s = 0; s < NT; ++s) kl[((rt * 2 + k2) * NT + s) * kFragLanes + lane] = t[s];
       }
+      lo = zero16();
       project_terms<DK, NSX, NW, false, WHOLE>(weights, own_rows, acc, lo);
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
@@ -444,6 +446,7 @@ __global__ __launch_bounds__(256, sizeof(TX) == 2 && DK <= 4 ? 2 : 1) void k_dec
     __syncthreads();
     floatx16 acc, lo, ph, df = zero16();
     // features of the other rows, the positions along the registers
+    lo = zero16();
     project_terms<DK, NSX, NW, true, WHOLE>(weights, other_rows, acc, lo);
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
@@ -471,7 +474,8 @@ __global__ __launch_bounds__(256, sizeof(TX) == 2 && DK <= 4 ? 2 : 1) void k_dec
 #pragma unroll
       for (int e = 0; e < 16; ++e) df[e] = fmaf(sden[8 * (e >> 2) + 4 * lh + (e & 3)], one, df[e]);
     }
-    project_terms<DK, NSX, NW, false, WHOLE>(weights, own_rows, acc, lo);
+    lo = zero16();
+      project_terms<DK, NSX, NW, false, WHOLE>(weights, own_rows, acc, lo);
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
       const int l = 8 * (e >> 2) + 4 * lh + (e & 3);
@@ -539,6 +543,7 @@ template <typename TX, bool ELU>
 hipError_t by_width(const DecayArgs& a, hipStream_t st) {
   if (a.d <= 32) return go<TX, 2, ELU>(a, st);
   if (a.d <= 64) return go<TX, 4, ELU>(a, st);
+  if (a.d <= 96) return go<TX, 6, ELU>(a, st);
   return go<TX, 8, ELU>(a, st);
 }
 

@@ -17,7 +17,7 @@ namespace krpe {
 // while those at hand are worked on.
 // NT: terms of features and values; NP: of P and the state.
 template <typename TX, int DK, int NT, int NP, bool ELU>
-__global__ __launch_bounds__(256, DK <= 4 ? 2 : 1) void k_decay_out(DecayArgs a) {
+__device__ __forceinline__ void decay_out(const DecayArgs& a, int block) {
   constexpr bool WHOLE = sizeof(TX) == 4;
   constexpr int NSX = kTermsX<TX>, DT = DK / 2, NW = 2;
   constexpr bool KROWS = WHOLE;  // the rows of k through LDS, where registers are short
@@ -27,13 +27,13 @@ __global__ __launch_bounds__(256, DK <= 4 ? 2 : 1) void k_decay_out(DecayArgs a)
   uint4* const kl = sl + DT * 2 * NP * kFragLanes;   // [4][2][NT][64]
   uint4* const xl = kl + 8 * NT * kFragLanes;        // KROWS: k [4][DK][NSX][64], each wave its own
   // the values' columns [4][DT][2][NT][64]: from the start, or after the features in their place
-  constexpr bool EARLY = !WHOLE;
+  constexpr bool EARLY = !KROWS;
   uint4* const vl = EARLY ? kl + 8 * NT * kFragLanes : smem;
   __shared__ __align__(16) float sden[32];
   __shared__ int odd;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lr = lane & 31, lh = lane >> 5;
-  const int ch = blockIdx.x % a.nchunk, bh = blockIdx.x / a.nchunk, b = bh / a.H, h = bh % a.H, d = a.d;
+  const int ch = block % a.nchunk, bh = block / a.nchunk, b = bh / a.H, h = bh % a.H, d = a.d;
   const int p0 = ch * kChunk, rows = rows_of(a.lens, b, a.n), cnt = min(kChunk, rows - p0);
   if (cnt <= 0) return;
   const int slot = a.state ? slot_of(a.slots, b, a.B, a.nslots) : kStateNone;
@@ -49,7 +49,7 @@ __global__ __launch_bounds__(256, DK <= 4 ? 2 : 1) void k_decay_out(DecayArgs a)
   const bool has = state.any();
   // the row tile of a wave: the last ones have the most to do, so that every other 256 work-groups
   // (those that share a CU) have them the other way round
-  const int rt = (blockIdx.x >> 8) & 1 ? 3 - wave : wave;
+  const int rt = (block >> 8) & 1 ? 3 - wave : wave;
   const int i = 32 * rt + lr;
   const size_t from = base + static_cast<size_t>(p0) * d;
   const Rows<TX> qr(static_cast<const TX*>(a.q) + from, cnt, d), kr(static_cast<const TX*>(a.k) + from, cnt, d),
@@ -106,6 +106,7 @@ __global__ __launch_bounds__(256, DK <= 4 ? 2 : 1) void k_decay_out(DecayArgs a)
     floatx16 acc, lo, ph;
     const bool part = f0 + 32 > a.M;  // uniform: features past M weigh nothing
     auto features = [&](auto&& rows, const RowFactors& o) {
+      lo = zero16();
       project_terms<DK, NSX, NW, false, WHOLE>(weights, rows, acc, lo);
 #pragma unroll
       for (int e = 0; e < 16; ++e) ph[e] = feature<ELU, WHOLE>(acc[e], WHOLE ? lo[e] : 0.f, o.r, o.c);
@@ -241,29 +242,57 @@ __global__ __launch_bounds__(256, DK <= 4 ? 2 : 1) void k_decay_out(DecayArgs a)
     }
 }
 
+template <typename TX, int DK, int NT, int NP, bool ELU>
+__global__ __launch_bounds__(256, DK <= 4 ? 2 : 1) void k_decay_out(DecayArgs a) {
+  decay_out<TX, DK, NT, NP, ELU>(a, blockIdx.x);
+}
+
+// Prompts of one chunk from empty states: their outputs need no sums, so that both are one launch, of
+// as many work-groups for each head as there are groups of 128 features and one more (12 heads, n = 128,
+// 64 features: 21 us of two dependent launches).
+template <typename TX, int DK, int NT, int NP, bool ELU>
+__global__ __launch_bounds__(256) void k_decay_short(DecayArgs a) {
+  if (blockIdx.y == 0)
+    decay_out<TX, DK, NT, NP, ELU>(a, blockIdx.x);
+  else
+    decay_states<TX, TX, DK, 3, NT, ELU, Sums::kForth, 4>(a, blockIdx.x, 0, blockIdx.y - 1);
+}
+
 namespace {
 
 template <typename TX, int DK, bool ELU>
 hipError_t go(const DecayArgs& a, hipStream_t st) {
   constexpr int NT = sizeof(TX) == 2 ? 1 : 3, NP = sizeof(TX) == 2 ? 2 : 3, DT = DK / 2;
   const int BH = a.B * a.H;
-  // (a single chunk from zeros whose state is not kept needs no sums)
-  if (a.state || a.nchunk > 1) launch_decay_states<TX, TX, DK, 3, NT, ELU, Sums::kForth>(a, st);
-  if (a.nchunk > 0) {
-    constexpr int NSX = kTermsX<TX>, NW = 2;
-    constexpr int feat = DK * NW + DT * 2 * NP + 8 * NT + (sizeof(TX) == 4 ? 4 * DK * NSX : 0), vals = 8 * DT * NT;
-    constexpr int lds = (sizeof(TX) == 2 ? feat + vals : feat > vals ? feat : vals) * 1024;
-    if constexpr (lds > 65536)
-      (void)hipFuncSetAttribute(reinterpret_cast<const void*>(&k_decay_out<TX, DK, NT, NP, ELU>),
-                                hipFuncAttributeMaxDynamicSharedMemorySize, lds);
-    hipLaunchKernelGGL((k_decay_out<TX, DK, NT, NP, ELU>), dim3(static_cast<unsigned>(BH) * a.nchunk), dim3(256), lds, st, a);
+  constexpr int NSX = kTermsX<TX>, NW = 2;
+  constexpr bool krows = sizeof(TX) == 4;  // (k_decay_out's KROWS)
+  constexpr int feat = DK * NW + DT * 2 * NP + 8 * NT + (krows ? 4 * DK * NSX : 0), vals = 8 * DT * NT;
+  constexpr int lds = (!krows ? feat + vals : feat > vals ? feat : vals) * 1024;
+  if constexpr (lds > 65536)
+    (void)hipFuncSetAttribute(reinterpret_cast<const void*>(&k_decay_out<TX, DK, NT, NP, ELU>),
+                              hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+  const bool one = a.nchunk == 1 && (!a.state || a.fresh);
+  if constexpr (DK <= 4) {
+    // (where all of them are resident at once)
+    if (one && a.state && BH * (1 + (a.Mp / 32 + 3) / 4) <= 256) {
+      if constexpr (lds + 49152 > 65536)
+        (void)hipFuncSetAttribute(reinterpret_cast<const void*>(&k_decay_short<TX, DK, NT, NP, ELU>),
+                                  hipFuncAttributeMaxDynamicSharedMemorySize, lds);
+      hipLaunchKernelGGL((k_decay_short<TX, DK, NT, NP, ELU>), dim3(BH, 1 + (a.Mp / 32 + 3) / 4), dim3(256), lds, st, a);
+      return hipGetLastError();
+    }
   }
+  // (a single chunk from zeros whose state is not kept needs no sums)
+  if (a.state || !one) launch_decay_states<TX, TX, DK, 3, NT, ELU, Sums::kForth>(a, st);
+  if (a.nchunk > 0)
+    hipLaunchKernelGGL((k_decay_out<TX, DK, NT, NP, ELU>), dim3(static_cast<unsigned>(BH) * a.nchunk), dim3(256), lds, st, a);
   return hipGetLastError();
 }
 template <typename TX, bool ELU>
 hipError_t by_width(const DecayArgs& a, hipStream_t st) {
   if (a.d <= 32) return go<TX, 2, ELU>(a, st);
   if (a.d <= 64) return go<TX, 4, ELU>(a, st);
+  if (a.d <= 96) return go<TX, 6, ELU>(a, st);
   return go<TX, 8, ELU>(a, st);
 }
 
@@ -278,6 +307,8 @@ hipError_t launch_decay_commit(bool bf16, bool elu, const DecayArgs& a, hipStrea
       launch_decay_states<TX, TX, 2, 3, NV, ELU, Sums::kPath>(a, st);
     else if (a.d <= 64)
       launch_decay_states<TX, TX, 4, 3, NV, ELU, Sums::kPath>(a, st);
+    else if (a.d <= 96)
+      launch_decay_states<TX, TX, 6, 3, NV, ELU, Sums::kPath>(a, st);
     else
       launch_decay_states<TX, TX, 8, 3, NV, ELU, Sums::kPath>(a, st);
   };

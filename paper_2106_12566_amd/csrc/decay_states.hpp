@@ -31,16 +31,16 @@ __device__ __forceinline__ int path_rows(const int* __restrict__ path, int P, in
 // 32 PB of them at a time and fetched that far ahead.
 // NP, NV: terms of the features and of the values.
 template <typename TX, typename TV, int DK, int NP, int NV, bool ELU, Sums MODE, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, DK <= 4 ? 2 : 1) void k_decay_states(DecayArgs a) {
+__device__ __forceinline__ void decay_states(const DecayArgs& a, int bh, int seg, int group) {
   constexpr bool BACK = MODE == Sums::kBack, PATH = MODE == Sums::kPath, WHOLE = sizeof(TX) == 4;
-  constexpr int NSX = kTermsX<TX>, NW = WHOLE ? 2 : 3, DT = DK / 2, PB = WHOLE || DK == 8 || PATH ? 2 : 4;
+  constexpr int NSX = kTermsX<TX>, NW = WHOLE ? 2 : 3, DT = DK / 2, PB = WHOLE || DK >= 6 || PATH ? 2 : 4;
   constexpr int BPW = (PB + WAVES - 1) / WAVES;  // blocks of x that a wave stages
   __shared__ __align__(16) uint4 xl[PB * DK * NSX * kFragLanes], vl[PB * DT * 2 * NV * kFragLanes];
-  __shared__ __align__(16) float fr[32 * PB], fc[32 * PB], fd[BACK ? 32 * PB : 4];
+  __shared__ __align__(16) float fr[32 * PB], fc[32 * PB], ff[32 * PB], fd[BACK ? 32 * PB : 4];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lr = lane & 31, lh = lane >> 5;
-  const int seg = blockIdx.y, bh = blockIdx.x, b = bh / a.H, h = bh % a.H, d = a.d, M = a.M, Mp = a.Mp;
-  const int l = (blockIdx.z * WAVES + wave) * 32 + lr;
+  const int b = bh / a.H, h = bh % a.H, d = a.d, M = a.M, Mp = a.Mp;
+  const int l = (group * WAVES + wave) * 32 + lr;
   const int* __restrict__ path = PATH ? a.path + static_cast<size_t>(b) * a.P : nullptr;
   const int rows = PATH ? path_rows(path, a.P, a.n) : rows_of(a.lens, b, a.n);
   const bool whole = PATH || a.nseg == 1;  // uniform
@@ -147,7 +147,7 @@ __global__ __launch_bounds__(64 * WAVES, DK <= 4 ? 2 : 1) void k_decay_states(De
               o.c = r < cnt ? __builtin_amdgcn_exp2f(e) : 0.f;
             else
               o.c = r < cnt ? o.c + e : -INFINITY;
-            fr[32 * blk + lr] = o.r, fc[32 * blk + lr] = o.c;
+            fr[32 * blk + lr] = o.r, fc[32 * blk + lr] = o.c, ff[32 * blk + lr] = o.f;
             if constexpr (BACK) fd[32 * blk + lr] = rd[i];
           }
         }
@@ -170,6 +170,11 @@ __global__ __launch_bounds__(64 * WAVES, DK <= 4 ? 2 : 1) void k_decay_states(De
 #pragma unroll 1
       for (int blk = 0; blk < PB && q0 + 32 * blk < cnt; ++blk) {
         floatx16 acc, lo, ph;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const float4 f4 = *reinterpret_cast<const float4*>(ff + 32 * blk + 8 * g + 4 * lh);
+          lo[4 * g] = f4.x, lo[4 * g + 1] = f4.y, lo[4 * g + 2] = f4.z, lo[4 * g + 3] = f4.w;
+        }
         project_terms<DK, NSX, NW, true, WHOLE>(
             [&](int ks, uint4(&w)[NW]) {
 #pragma unroll
@@ -183,7 +188,8 @@ __global__ __launch_bounds__(64 * WAVES, DK <= 4 ? 2 : 1) void k_decay_states(De
           const float r_[4] = {r4.x, r4.y, r4.z, r4.w}, c_[4] = {c4.x, c4.y, c4.z, c4.w};
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
-            const float y = feature<ELU, WHOLE>(acc[4 * g + j], WHOLE ? lo[4 * g + j] : 0.f, r_[j], c_[j]);
+            const float s = WHOLE ? acc[4 * g + j] : acc[4 * g + j] + lo[4 * g + j];
+            const float y = feature<ELU, WHOLE>(s, WHOLE ? lo[4 * g + j] : 0.f, r_[j], c_[j]);
             ph[4 * g + j] = ELU ? y * c_[j] : y;
           }
         }
@@ -218,6 +224,11 @@ __global__ __launch_bounds__(64 * WAVES, DK <= 4 ? 2 : 1) void k_decay_states(De
     store((BACK ? a.totb : a.tot) + (static_cast<size_t>(bh) * a.nseg + seg) * cells, Mp);
   else if (slot >= 0)
     store(st, M);
+}
+
+template <typename TX, typename TV, int DK, int NP, int NV, bool ELU, Sums MODE, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, DK <= 4 || (DK == 6 && WAVES == 4 && sizeof(TX) == 2) ? 2 : 1) void k_decay_states(DecayArgs a) {
+  decay_states<TX, TV, DK, NP, NV, ELU, MODE, WAVES>(a, blockIdx.x, blockIdx.y, blockIdx.z);
 }
 
 // The state before each segment (kBack: after it) in place of the segment's sums, and the one

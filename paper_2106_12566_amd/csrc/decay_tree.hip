@@ -26,7 +26,7 @@ __global__ __launch_bounds__(64 * kSplit * RT, sizeof(TX) == 2 && DK <= 4 ? 2 : 
   constexpr bool WHOLE = sizeof(TX) == 4;
   constexpr int THREADS = 64 * kSplit * RT, NX = sizeof(TX) / 2;
   constexpr int NSX = kTermsX<TX>, DT = DK / 2, NW = 2, NP = RT == 1 ? 1 : 3;
-  constexpr int CG = DT < 2 ? DT : 2;  // column tiles summed at a time
+  constexpr int CG = DT % 2 ? 1 : 2;  // column tiles summed at a time
   // first the rows as they are [k, q][RT][DK][NX][64]; then the partial sums: S tiles [kSplit][NP], Z
   // [kSplit][RT][CG] a group of columns at a time
   constexpr int kRowsX = 2 * RT * DK * NX * 64, kTiles = NP > RT * CG ? NP : RT * CG, kPart = kSplit * kTiles * 16 * 16;
@@ -61,7 +61,7 @@ __global__ __launch_bounds__(64 * kSplit * RT, sizeof(TX) == 2 && DK <= 4 ? 2 : 
   const Rows<float> sr(st ? st : a.state, st ? d + 1 : 0, M);  // (no state: zeros)
   const bool vec = M % 4 == 0;
   // (a column tile's share is asked for when the one before is used where registers are short)
-  constexpr bool LATE = DK == 8 || (WHOLE && DK == 4);
+  constexpr bool LATE = DK >= 6 || (WHOLE && DK == 4);
   float s8[LATE ? 1 : DT][2][8], sd[16];
   auto fetch_state = [&](int f0, int ct, float(&s)[2][8]) {
 #pragma unroll
@@ -150,7 +150,7 @@ __global__ __launch_bounds__(64 * kSplit * RT, sizeof(TX) == 2 && DK <= 4 ? 2 : 
     // features of a row tile (lane: row; features along the registers), zeros past M
     auto features = [&](int w, int t, floatx16& ph, uint4(&p)[2][NT]) {
       const float scale = fx[w][32 * t + lr];
-      floatx16 acc, lo;
+      floatx16 acc, lo = zero16();
       project_terms<DK, NSX, NW, false, WHOLE>(
           [&](int ks, uint4(&y)[NW]) {
 #pragma unroll
@@ -315,6 +315,7 @@ template <typename TX, bool ELU>
 hipError_t by_width(const PoolArgs& a, hipStream_t st) {
   if (a.d <= 32) return go<TX, 2, ELU>(a, st);
   if (a.d <= 64) return go<TX, 4, ELU>(a, st);
+  if (a.d <= 96) return go<TX, 6, ELU>(a, st);
   return go<TX, 8, ELU>(a, st);
 }
 }  // namespace
