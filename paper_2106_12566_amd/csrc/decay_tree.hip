@@ -5,11 +5,17 @@
 //   num_t | den_t = e^{-rate (dep_t + 1)} A phi(q_t)
 //                 + sum_{a in anc(t)} e^{-rate (dep_t - dep_a)} (phi(q_t) . phi(k_a)) [v_a | 1]
 //
-// A work-group is one sequence and head.  Four waves for each row tile of 32
-// nodes split the features; what a wave needs of the state goes straight from
-// memory into its operands, asked for before any row is worked on.  S = phi(K)
-// phi(Q)^T and A phi(Q) leave the waves as partial sums, which are added
-// through LDS in a fixed order.
+// A work-group is one sequence and head, four waves: a row tile of 32 nodes or
+// two, whose waves split the features.  What a wave needs of the state goes
+// straight from memory into its operands, asked for before any row is worked
+// on.  S = phi(K) phi(Q)^T and A phi(Q) leave the waves as partial sums, which
+// are added through LDS in a fixed order.
+//
+// Bound by latency: the loads, the features, two sums through LDS.  64 x 16
+// heads, 64 nodes, 256 features, d = 64 (100 MB in and out, 20 us at a plain
+// copy's rate): 52 us, two work-groups on a CU, one of which loads while the
+// other computes; with four waves for each of the two row tiles, one
+// work-group on a CU, 69 us (a single sequence: 17.6 and 17.1 us).
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
@@ -18,10 +24,8 @@
 
 namespace krpe {
 
-constexpr int kSplit = 4;  // waves of a row tile
-
-// RT: row tiles (T <= 32 RT); NT: terms of features and values; NPP: of P and the state.
-template <typename TX, int DK, int NT, int NPP, int RT, bool ELU>
+// kSplit: waves of a row tile; RT: row tiles (T <= 32 RT); NT: terms of features and values; NPP: of P and the state.
+template <typename TX, int DK, int NT, int NPP, int RT, int kSplit, bool ELU>
 __global__ __launch_bounds__(64 * kSplit * RT, sizeof(TX) == 2 && DK <= 4 ? 2 : 1) void k_decay_tree(PoolArgs a) {
   constexpr bool WHOLE = sizeof(TX) == 4;
   constexpr int THREADS = 64 * kSplit * RT, NX = sizeof(TX) / 2;
@@ -306,9 +310,9 @@ hipError_t go(const PoolArgs& a, hipStream_t st) {
   constexpr int NT = sizeof(TX) == 2 ? 1 : 3, NP = sizeof(TX) == 2 ? 2 : 3;
   const dim3 grid(static_cast<unsigned>(a.B) * a.H);
   if (a.T <= 32)
-    hipLaunchKernelGGL((k_decay_tree<TX, DK, NT, NP, 1, ELU>), grid, dim3(64 * kSplit), 0, st, a);
+    hipLaunchKernelGGL((k_decay_tree<TX, DK, NT, NP, 1, 4, ELU>), grid, dim3(256), 0, st, a);
   else
-    hipLaunchKernelGGL((k_decay_tree<TX, DK, NT, NP, 2, ELU>), grid, dim3(128 * kSplit), 0, st, a);
+    hipLaunchKernelGGL((k_decay_tree<TX, DK, NT, NP, 2, 2, ELU>), grid, dim3(256), 0, st, a);
   return hipGetLastError();
 }
 template <typename TX, bool ELU>
