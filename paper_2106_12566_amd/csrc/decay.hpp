@@ -312,14 +312,14 @@ struct WeightTile {
     for (int i = 0; i < N; ++i) {
       const int e = threadIdx.x + 256 * i;
       if (N * 256 > 64 * DK && e >= 64 * DK) return;
-      load_weights<ELU>(W, f0 + e / (2 * DK), 8 * (e % (2 * DK)), v[i]);
+      load_weights<ELU>(W, f0 + (e & 31), 8 * (e >> 5), v[i]);
     }
   }
   __device__ __forceinline__ void put(uint4* __restrict__ wf) const {
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-      const int e = threadIdx.x + 256 * i, fl = e / (2 * DK), c = e % (2 * DK);
-      if (N * 256 > 64 * DK && fl >= 32) return;
+      const int e = threadIdx.x + 256 * i, fl = e & 31, c = e >> 5;
+      if (N * 256 > 64 * DK && e >= 64 * DK) return;
       uint4 t[NW];
       weight_terms<NW, WHOLE>(v[i], t);
       uint4* __restrict__ o = wf + (c >> 1) * NW * kFragLanes + (c & 1) * 32 + fl;
@@ -540,7 +540,7 @@ struct StateTile {
           x[n][t] = r.one(c < d ? r.at(c) + 4u * (f0 + l) : kOut);
         }
       } else {
-        const int c = e >> 2, ks = (e >> 1) & 1, half = e & 1;
+        const int c = 32 * (e >> 7) + (e & 31), ks = (e >> 6) & 1, half = (e >> 5) & 1;
         const uint32_t at = c < d ? r.at(c) + 4u * (f0 + 16 * ks + 4 * half) : kOut;
         const uint4 u = r.b128(at), w = r.b128(at + 32);
         x[n][0] = __uint_as_float(u.x), x[n][1] = __uint_as_float(u.y), x[n][2] = __uint_as_float(u.z), x[n][3] = __uint_as_float(u.w);
@@ -568,7 +568,7 @@ struct StateTile {
       if constexpr (COLUMNS)
         at = (e >> 6) * NT * kFragLanes + (e & 63);
       else
-        at = (((e >> 7) * 2 + ((e >> 1) & 1)) * NT) * kFragLanes + 32 * (e & 1) + ((e >> 2) & 31);
+        at = (((e >> 7) * 2 + ((e >> 6) & 1)) * NT) * kFragLanes + (e & 63);
 #pragma unroll
       for (int s = 0; s < NT; ++s) sl[at + s * kFragLanes] = make_uint4(q[0][s], q[1][s], q[2][s], q[3][s]);
     }

@@ -28,7 +28,7 @@ struct RowTile {
   __device__ __forceinline__ void fetch(const Rows<T>& x) {
 #pragma unroll
     for (int n = 0; n < DK; ++n) {
-      const int e = threadIdx.x + 256 * n, half = e & 1, ks = (e >> 1) % DK, r = e / (2 * DK);
+      const int e = threadIdx.x + 256 * n, r = e & 127, half = (e >> 7) & 1, ks = e >> 8;
       u[n][0].load(x, x.at(r), 16 * ks + 4 * half);
       u[n][1].load(x, x.at(r), 16 * ks + 4 * half + 8);
     }
@@ -37,7 +37,7 @@ struct RowTile {
   __device__ __forceinline__ void put(uint4* __restrict__ f) const {
 #pragma unroll
     for (int n = 0; n < DK; ++n) {
-      const int e = threadIdx.x + 256 * n, half = e & 1, ks = (e >> 1) % DK, r = e / (2 * DK);
+      const int e = threadIdx.x + 256 * n, r = e & 127, half = (e >> 7) & 1, ks = e >> 8;
       float v[4], w[4];
       u[n][0].values(v);
       u[n][1].values(w);
