@@ -102,11 +102,12 @@ __global__ __launch_bounds__(256, 4) void k_decay_step(PoolArgs a) {
   slot = check_slot(a.slots, slot, b, a.B);
   const float w = decay(rate_log2(a.rate[h]), 1);
   __syncthreads();
-  for (int l = 4 * lane; l < M4 || l < 4 * L; l += 4 * L) {  // (all lanes go round together)
+  for (int l0 = 0; l0 < M4; l0 += 4 * L) {  // (all lanes go round together)
+    const int l = l0 + 4 * lane;
     float4 gq = make_float4(0.f, 0.f, 0.f, 0.f), gk = gq;
     if (l < M) gq = *reinterpret_cast<const float4*>(fq + l), gk = *reinterpret_cast<const float4*>(fk + l);
     for (int p = 0; p * K * R <= d; ++p) {
-      if (p || l >= 4 * L) fetch(l, p);
+      if (p || l0) fetch(l, p);
       float s[K];
 #pragma unroll
       for (int i = 0; i < K; ++i) {

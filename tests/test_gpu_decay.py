@@ -55,6 +55,8 @@ PROMPTS = [
     (1, 3, 2000, 64, 64, "f32", "prf", False, True),
     (1, 2, 4001, 64, 128, "bf16", "prf", True, False),
     (3, 2, 700, 40, 48, "f32", "prf", False, False),
+    (2, 2, 100, 72, 90, "bf16", "prf", True, False),
+    (1, 2, 390, 96, 300, "f32", "prf", False, True),
 ]
 
 
@@ -159,6 +161,8 @@ GRADS = [
     (1, 2, 300, 64, 64, "bf16", "elu", True),
     (1, 2, 1500, 32, 64, "f32", "prf", False),
     (1, 1, 2600, 64, 64, "bf16", "prf", False),
+    (1, 2, 270, 72, 90, "bf16", "prf", True),
+    (1, 1, 200, 96, 300, "f32", "prf", False),
 ]
 
 
@@ -207,6 +211,8 @@ STEPS = [
     (5, 3, 128, 256, "bf16", "prf", False),
     (2, 1, 128, 1024, "f32", "prf", False),
     (2, 2, 30, 77, "bf16", "prf", True),
+    (2, 2, 20, 300, "f32", "prf", False),     # features past 256 that do not fill a wave
+    (1, 2, 64, 513, "bf16", "prf", False),
     (4, 2, 65, 65, "f32", "elu", False),
     (40, 2, 64, 128, "bf16", "prf", False),
 ]
@@ -244,6 +250,8 @@ TREES = [
     (1, 1, 64, 128, 1024, "f32", "prf", False),
     (1, 2, 50, 65, 65, "bf16", "elu", True),
     (1, 2, 64, 100, 130, "bf16", "prf", False),
+    (1, 2, 40, 72, 90, "f32", "prf", True),
+    (1, 1, 20, 96, 300, "bf16", "prf", False),
 ]
 
 
