@@ -338,7 +338,7 @@ krpe_status_t krpe_attention_fwd_stats(const void* ws, size_t ws_bytes, int B, i
  *   is not finite makes what sees it not finite, and nothing else (gradients: its whole sequence
  *   and head).
  * - rate and integer arrays need 4-byte alignment, all others 16 bytes.
- * - 1 <= d <= 128, 1 <= m <= 1024; B H n < 2^31, no other limit of n.
+ * - 1 <= d <= 128, 1 <= m <= 1024; B H n < 2^31 and B H ceil(n / 128) < 2^24, no other limit of n.
  */
 
 /*

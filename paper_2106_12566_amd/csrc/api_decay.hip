@@ -2,6 +2,7 @@
 // validation on the host, workspace carving and the launches.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 #include <cstdint>
 #include <string>
@@ -70,6 +71,9 @@ krpe_status_t check_sizes(int B, int H, int n, int d, int m, unsigned flags, uns
   const long long bh = static_cast<long long>(B) * H;
   if (bh >= (1LL << 31) || (n > 0 && bh > ((1LL << 31) - 1) / n))
     return fail(KRPE_ERR_UNSUPPORTED, "B * H * n >= 2^31 is not supported");
+  // (a grid of 256-thread groups, one for each head's chunk)
+  if (bh * std::max(1, (n + kChunk - 1) / kChunk) >= (1LL << 24))
+    return fail(KRPE_ERR_UNSUPPORTED, "2^24 or more chunks of 128 positions are not supported");
   return KRPE_OK;
 }
 krpe_status_t check_dtype(int dt) {

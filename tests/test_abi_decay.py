@@ -37,6 +37,7 @@ def test_fwd(lib):
     assert call(r=R + 2) == ALIGN and call(slots=I + 1) == ALIGN and call(lens=J + 2) == ALIGN
     assert call(B=-1) == SHAPE and call(n=-1) == SHAPE and call(d=0) == SHAPE and call(m=0) == SHAPE
     assert call(d=129) == UNSUP and call(m=1025) == UNSUP and call(n=1 << 30) == UNSUP
+    assert call(B=1 << 12, H=1 << 12, n=1) == UNSUP    # more chunks than a grid has groups
     assert call(flags=2) == UNSUP and call(flags=8) == UNSUP and call(flags=16) == UNSUP and call(flags=128) == UNSUP
     assert call(flags=4) == SHAPE                      # elu + 1 needs m == d
     assert call(dt=2) == DTYPE
