@@ -43,11 +43,6 @@ def _flags() -> list[str]:
     ]
 
 
-def command(out: str = LIB) -> list[str]:
-    """One hipcc run compiling and linking every source into `out`."""
-    return [hipcc(), *_flags(), "-shared", "-o", out, TOP, *SOURCES]
-
-
 def object_command(src: str, obj: str) -> list[str]:
     return [hipcc(), *_flags(), *(TOP_FLAGS if src == TOP else []), "-c", "-o", obj, src]
 

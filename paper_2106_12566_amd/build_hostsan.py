@@ -18,6 +18,7 @@ import glob
 import os
 import subprocess
 import sys
+from concurrent.futures import ThreadPoolExecutor
 
 from paper_2106_12566_amd import build
 
@@ -34,12 +35,24 @@ def runtime() -> str:
 
 
 def build_hostsan(out: str) -> str:
-    cmd = build.command(out)
-    cmd[cmd.index("-O3")] = "-O1"
-    cmd[1:1] = ["-g", *HOST_SANITIZERS.split()]
-    res = subprocess.run(cmd, capture_output=True, text=True)
-    if res.returncode != 0:
-        raise RuntimeError(f"hipcc failed ({res.returncode}):\n{res.stdout}\n{res.stderr}")
+    """Compile OUT.so, the sources side by side as in the product build; return its path."""
+    flags = ["-g", *HOST_SANITIZERS.split()]
+
+    def run(cmd: list[str]) -> None:
+        res = subprocess.run([cmd[0], *flags, *("-O1" if a == "-O3" else a for a in cmd[1:])], capture_output=True, text=True)
+        if res.returncode != 0:
+            raise RuntimeError(f"hipcc failed ({res.returncode}):\n{res.stdout}\n{res.stderr}")
+
+    sources = [build.TOP, *build.SOURCES]
+    objs = [f"{out}.{os.path.splitext(os.path.basename(s))[0]}.o" for s in sources]
+    try:
+        with ThreadPoolExecutor(max_workers=min(len(sources), os.cpu_count() or 1)) as pool:
+            list(pool.map(lambda so: run(build.object_command(*so)), zip(sources, objs)))
+        run(build.link_command(objs, out))
+    finally:
+        for o in objs:
+            if os.path.exists(o):
+                os.remove(o)
     return out
 
 
