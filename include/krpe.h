@@ -334,9 +334,8 @@ krpe_status_t krpe_attention_fwd_stats(const void* ws, size_t ws_bytes, int B, i
  *   kept after it.  A slot outside [-1, nslots), or one that two sequences of a call name, is
  *   refused on the device: these sequences' z is NaN and the pool stays as it was.
  * - features have to stay within fp32's range, as krpe_feature_map's (with fp32 q, k, v: |W| < 65504
- *   too).  A q, k or v element that
- *   is not finite makes what sees it not finite, and nothing else (gradients: its whole sequence
- *   and head).
+ *   too).  A q, k or v element that is not finite makes what sees it, at whatever weight, not
+ *   finite, and nothing else (gradients: its whole sequence and head).
  * - rate and integer arrays need 4-byte alignment, all others 16 bytes.
  * - 1 <= d <= 128, 1 <= m <= 1024; B H n < 2^31 and B H ceil(n / 128) < 2^24, no other limit of n.
  */
@@ -391,7 +390,7 @@ krpe_status_t krpe_decay_tree(const void* q, const void* k, const void* v, int q
 
 /*
  * Takes tokens path[b][0], path[b][1], .. of k, v [B, H, T, d] into the states, in that order, up
- * to the first entry outside [0, T) or P entries; T <= 65536.  path: [B, P] int32 (device).
+ * to the first entry outside [0, T) or P entries; T <= 65536, P < 2^30.  path: [B, P] int32 (device).
  */
 krpe_status_t krpe_decay_commit(const void* k, const void* v, int qkv_dtype, const int* path, const float* rate,
                                 const float* W, float* state, const int* slots, int nslots, int B, int H, int T,
@@ -401,6 +400,7 @@ krpe_status_t krpe_decay_commit(const void* k, const void* v, int qkv_dtype, con
  * state[dst[i]] = state[src[i]] for i < count <= KRPE_COPY_MAX, all at once: sources are as they
  * were before the call, also where moves overlap; src -1 clears; of moves to one slot the last
  * holds.  Moves with a slot outside the pool are left out.  src, dst: [count] int32 (device).
+ * H (d + 1) m < 2^31.
  */
 #define KRPE_COPY_MAX 256
 krpe_status_t krpe_decay_state_copy(float* state, const int* src, const int* dst, int count, int nslots, int H, int d,

@@ -14,6 +14,8 @@
 namespace krpe {
 namespace {
 
+int chunks(int n) { return static_cast<int>((static_cast<long long>(n) + kChunk - 1) / kChunk); }
+
 // A prompt's sums: chunks of 128 positions in nseg segments of segc chunks.
 struct DecayLayout {
   int nchunk, nseg, segc, Mp;
@@ -23,7 +25,7 @@ struct DecayLayout {
 DecayLayout decay_layout(long long BH, int n, int d, int m, size_t off) {
   DecayLayout L{};
   L.Mp = (m + 31) & ~31;
-  L.nchunk = (n + kChunk - 1) / kChunk;
+  L.nchunk = chunks(n);
   // The number of segments from the rounds of work-groups that the sums take: a group of 128
   // features and a segment each, two to a CU (one beyond 64 dimensions, twice as many of the
   // two-wave groups of up to 64 features), a chunk costing one unit, a group's start a half and
@@ -33,11 +35,10 @@ DecayLayout decay_layout(long long BH, int n, int d, int m, size_t off) {
   const long long slots = (d <= 64 ? 512 : 256) * (L.Mp <= 64 ? 2 : 1);
   double best = 0.0;
   L.nseg = 1, L.segc = L.nchunk > 1 ? L.nchunk : 1;
-  for (int segc = L.nchunk; segc >= 1; --segc) {
-    const int nseg = (L.nchunk + segc - 1) / segc;
-    if (nseg > 256) break;
+  for (int most = 1; most <= 256 && most <= L.nchunk; ++most) {
+    const int segc = (L.nchunk + most - 1) / most, nseg = (L.nchunk + segc - 1) / segc;
     const double cost = static_cast<double>((groups * nseg + slots - 1) / slots) * (segc + 0.5) + 0.05 * nseg;
-    if (segc == L.nchunk || cost < best) best = cost, L.nseg = nseg, L.segc = segc;
+    if (most == 1 || cost < best) best = cost, L.nseg = nseg, L.segc = segc;
   }
   const size_t cells = static_cast<size_t>(d + 1) * L.Mp * sizeof(float);
   L.tot = off;
@@ -72,7 +73,7 @@ krpe_status_t check_sizes(int B, int H, int n, int d, int m, unsigned flags, uns
   if (bh >= (1LL << 31) || (n > 0 && bh > ((1LL << 31) - 1) / n))
     return fail(KRPE_ERR_UNSUPPORTED, "B * H * n >= 2^31 is not supported");
   // (a grid of 256-thread groups, one for each head's chunk)
-  if (bh * std::max(1, (n + kChunk - 1) / kChunk) >= (1LL << 24))
+  if (bh * std::max(1, chunks(n)) >= (1LL << 24))
     return fail(KRPE_ERR_UNSUPPORTED, "2^24 or more chunks of 128 positions are not supported");
   return KRPE_OK;
 }
@@ -268,6 +269,7 @@ krpe_status_t krpe_decay_commit(const void* k, const void* v, int qkv_dtype, con
   if (krpe_status_t s = check_pool(qkv_dtype, rate, W, state, slots, nslots, B, H, T, d, m, flags)) return s;
   if (P < 0) return fail(KRPE_ERR_SHAPE, "negative size");
   if (T > 65536) return fail(KRPE_ERR_UNSUPPORTED, "more than 65536 tokens to choose from is not supported");
+  if (P >= 1 << 30) return fail(KRPE_ERR_UNSUPPORTED, "a path of 2^30 or more entries is not supported");
   const long long bh = static_cast<long long>(B) * H;
   if (bh * T == 0 || P == 0) return KRPE_OK;
   if (!k || !v || !path) return fail(KRPE_ERR_NULL, "k, v and path must be non-NULL");
@@ -291,8 +293,10 @@ krpe_status_t krpe_decay_commit(const void* k, const void* v, int qkv_dtype, con
 krpe_status_t krpe_decay_state_copy(float* state, const int* src, const int* dst, int count, int nslots, int H, int d,
                                     int m, void* stream) {
   clear_error();
-  if (krpe_status_t s = check_sizes(nslots, H, 0, d, m, 0u, 0u)) return s;
-  if (count < 0) return fail(KRPE_ERR_SHAPE, "negative size");
+  if (krpe_status_t s = check_sizes(1, 1, 0, d, m, 0u, 0u)) return s;
+  if (nslots < 0 || H < 0 || count < 0) return fail(KRPE_ERR_SHAPE, "negative size");
+  if (static_cast<long long>(H) * (d + 1) * m >= (1LL << 31))
+    return fail(KRPE_ERR_UNSUPPORTED, "a slot of 2^31 or more elements is not supported");
   if (count > KRPE_COPY_MAX) return fail(KRPE_ERR_UNSUPPORTED, "more than 256 moves in a call are not supported");
   if (count == 0 || nslots == 0 || H == 0) return KRPE_OK;
   if (!state || !src || !dst) return fail(KRPE_ERR_NULL, "state, src and dst must be non-NULL");

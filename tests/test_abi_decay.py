@@ -38,6 +38,7 @@ def test_fwd(lib):
     assert call(B=-1) == SHAPE and call(n=-1) == SHAPE and call(d=0) == SHAPE and call(m=0) == SHAPE
     assert call(d=129) == UNSUP and call(m=1025) == UNSUP and call(n=1 << 30) == UNSUP
     assert call(B=1 << 12, H=1 << 12, n=1) == UNSUP    # more chunks than a grid has groups
+    assert call(B=1, H=1, n=(1 << 31) - 1) == UNSUP and call(B=1, H=1, n=(1 << 31) - 129, wb=0) == WS
     assert call(flags=2) == UNSUP and call(flags=8) == UNSUP and call(flags=16) == UNSUP and call(flags=128) == UNSUP
     assert call(flags=4) == SHAPE                      # elu + 1 needs m == d
     assert call(dt=2) == DTYPE
@@ -99,6 +100,7 @@ def test_pool_calls(lib):
         assert call(z=Q) == ALIAS and call(z=S) == ALIAS
     assert tree(T=65) == UNSUP and tree(T=-1) == SHAPE and tree(T=0) == OK and tree(par=None) == NULL
     assert commit(P=-1) == SHAPE and commit(P=0) == OK and commit(path=None) == NULL
+    assert commit(P=1 << 30) == UNSUP and commit(T=65537) == UNSUP
 
 
 def test_state_copy(lib):
@@ -109,8 +111,10 @@ def test_state_copy(lib):
     assert call(s=S + 4) == ALIGN and call(src=I + 1) == ALIGN
     assert call(count=-1) == SHAPE and call(ns=-1) == SHAPE
     assert call(count=krpe.COPY_MAX + 1) == UNSUP and call(d=200) == UNSUP
+    assert call(H=1 << 24, d=128, m=1024) == UNSUP     # a slot of 2^31 elements
     assert call(s=I - 256) == ALIAS
     assert call(count=0) == OK and call(ns=0) == OK
+    assert call(ns=1 << 20, H=16, count=0) == OK
 
 
 def test_binding_refuses(lib):
