@@ -61,31 +61,30 @@ __device__ __forceinline__ float decay(float rl, int dist) { return __builtin_am
 
 // The weights e^{-rate dist} of a 32 x 32 result's rows: dist = sign (i - j) for the lane's row i and rows
 // j = base + 8 (e / 4) + 4 lh + e % 4 along the registers; zero below 0 (EDGE: where that can be).
-// As products of a weight for each four rows and one of four that all share, which a rate of 40 bits
-// a position keeps in range; beyond, where the next position weighs less than 2^-40, only dist 0 counts.
+// There each by itself; elsewhere as products of the weight of the nearest of each four rows and one of
+// four that all share, which are in range wherever the weight is.
 struct TileWeights {
   float rl;
   int sign;
-  bool self;  // uniform
   float t[4];
-  __device__ __forceinline__ TileWeights(float rl_, int sign_) : rl(rl_ > 40.f ? 40.f : rl_), sign(sign_), self(rl_ > 40.f) {
+  __device__ __forceinline__ TileWeights(float rl_, int sign_) : rl(rl_), sign(sign_) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) t[j] = decay(rl, -sign * j);
+    for (int j = 0; j < 4; ++j) t[j] = decay(rl, sign > 0 ? 3 - j : j);
   }
   template <bool EDGE>
   __device__ __forceinline__ void apply(floatx16& x, int i, int base) const {
     const int d0 = sign * (i - base - 4 * static_cast<int>((threadIdx.x & 63) >> 5));
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
-      const float w = self ? 0.f : decay(rl, d0 - sign * 8 * g);
+      const float w = EDGE ? 0.f : decay(rl, d0 - sign * 8 * g - (sign > 0 ? 3 : 0));
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const float y = x[4 * g + j] * (w * t[j]);
         if constexpr (EDGE) {
           const int dist = d0 - sign * (8 * g + j);
+          const float y = x[4 * g + j] * decay(rl, dist);
           x[4 * g + j] = dist > 0 ? y : (dist == 0 ? x[4 * g + j] : 0.f);
         } else {
-          x[4 * g + j] = y;
+          x[4 * g + j] *= w * t[j];
         }
       }
     }

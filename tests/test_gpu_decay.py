@@ -55,6 +55,11 @@ PROMPTS = [
     (1, 3, 2000, 64, 64, "f32", "prf", False, True),
     (1, 2, 4001, 64, 128, "bf16", "prf", True, False),
     (3, 2, 700, 40, 48, "f32", "prf", False, False),
+    (40, 3, 300, 16, 24, "f32", "prf", False, True),   # more chunks than CUs
+    (40, 3, 300, 16, 24, "bf16", "prf", False, False),
+    (32, 4, 40, 16, 24, "bf16", "prf", False, False),  # one chunk from empty states: one launch,
+    (65, 3, 40, 16, 24, "bf16", "prf", False, False),  # and two
+    (43, 3, 128, 33, 160, "f32", "prf", False, False),
     (2, 2, 100, 72, 90, "bf16", "prf", True, False),
     (1, 2, 390, 96, 300, "f32", "prf", False, True),
 ]
@@ -81,7 +86,7 @@ def test_prompt(gpu_lib, B, H, n, d, m, dt, features, nprf, with_state):
         assert torch.equal(alone, z)      # the state that is kept changes nothing
 
 
-@pytest.mark.parametrize("rates", [[0.0, 1e-4], [INF, 50.0], [0.02, 3.0], [-0.01, 0.0]])
+@pytest.mark.parametrize("rates", [[0.0, 1e-4], [INF, 50.0], [0.02, 3.0], [-0.01, 0.0], [24.0, 41.0]])
 def test_rates(gpu_lib, rates):
     _say("rates", rates)
     c = Case(1, 2, 400, 16, 24, rates=rates)
@@ -89,6 +94,35 @@ def test_rates(gpu_lib, rates):
     z = gpu_lib.decay_attention_fwd(c.q, c.k, c.v, c.rate, c.W, state=c.state)
     for h in range(2):
         want, scale, last, lscale = ref.prompt(*c.head(0, h), state=before[0, h])
+        assert ref.excess(z[0, h], want, scale, z.dtype) <= 1.0
+        assert ref.excess(c.state[0, h], last, lscale, torch.float32, ref.STATE_DELTA) <= 1.0
+
+
+def test_next_positions_of_little_weight(gpu_lib):
+    """Keys that match a query badly beside one that does, three positions before at 32 bits each."""
+    _say("little weight")
+    n, d = 128, 16
+    c = Case(1, 1, n, d, 8, rates=[32 * float(np.log(2.0))])
+    x = torch.zeros(n, d, device="cuda")
+    x[:, 0] = torch.tensor([-7.0, -7.0, -7.0, 7.0], device="cuda").repeat(n // 4)
+    c.k[0, 0], c.q[0, 0] = x, x[3]
+    c.W.fill_(0.0)
+    c.W[0, :, 0] = 7.0        # phi(q) . phi(k): 1 or, for the others, e^-98 = 2^-141 of it
+    z = gpu_lib.decay_attention_fwd(c.q, c.k, c.v, c.rate, c.W)
+    # a matching key and the three rows after it, which it weighs 2^-32, 2^-64 and 2^-96: the others 2^-45 of that at most
+    want = c.v[0, 0, 3:127].double().view(31, 4, d)[:, :1]
+    assert float((z[0, 0, 3:127].view(31, 4, d) - want).abs().max()) <= 4e-5 * float(want.abs().max())
+
+
+@pytest.mark.parametrize("size", [3e-7, 3e-5])
+def test_small_projections(gpu_lib, size):
+    """W below what its operands' type holds without loss: phi is as near as elsewhere."""
+    _say("small W", size)
+    c = Case(1, 2, 200, 64, 64, rates=[3.0, 2.0])
+    c.W.mul_(size)
+    z = gpu_lib.decay_attention_fwd(c.q, c.k, c.v, c.rate, c.W, state=c.state, fresh=True)
+    for h in range(2):
+        want, scale, last, lscale = ref.prompt(*c.head(0, h))
         assert ref.excess(z[0, h], want, scale, z.dtype) <= 1.0
         assert ref.excess(c.state[0, h], last, lscale, torch.float32, ref.STATE_DELTA) <= 1.0
 
@@ -161,6 +195,8 @@ GRADS = [
     (1, 2, 300, 64, 64, "bf16", "elu", True),
     (1, 2, 1500, 32, 64, "f32", "prf", False),
     (1, 1, 2600, 64, 64, "bf16", "prf", False),
+    (40, 3, 300, 16, 24, "f32", "prf", False),         # more chunks than CUs
+    (40, 3, 300, 16, 24, "bf16", "prf", False),
     (1, 2, 270, 72, 90, "bf16", "prf", True),
     (1, 1, 200, 96, 300, "f32", "prf", False),
 ]
