@@ -248,8 +248,10 @@ __global__ __launch_bounds__(256, DK <= 4 ? 2 : 1) void k_decay_out(DecayArgs a)
 }
 
 // Prompts of one chunk from empty states: their outputs need no sums, so that both are one launch, of
-// as many work-groups for each head as there are groups of 128 features and one more (12 heads, n = 128,
-// 64 features: 21 us of two dependent launches).
+// as many work-groups for each head as there are groups of 128 features and one more.  One launch and
+// two, n = 128, d = 64, us: 12 heads, bf16, 64 features 10.4 and 19.4; 128 heads 11.2 and 20.0; 192 heads
+// (384 work-groups) 20.1 and 20.4; 256 features, 128 heads (384) 21.3 and 27.1, fp32 32.5 and 41.9; 192
+// heads (576) 31.1 and 30.5, fp32 44.6 and 46.7; 256 heads (768) 38.7 and 31.4, fp32 56.5 and 47.9.
 template <typename TX, int DK, int NT, int NP, bool ELU>
 __global__ __launch_bounds__(256) void k_decay_short(DecayArgs a) {
   if (blockIdx.y == 0)
@@ -273,8 +275,7 @@ hipError_t go(const DecayArgs& a, hipStream_t st) {
                               hipFuncAttributeMaxDynamicSharedMemorySize, lds);
   const bool one = a.nchunk == 1 && (!a.state || a.fresh);
   if constexpr (DK <= 4) {
-    // (where all of them are resident at once)
-    if (one && a.state && BH * (1 + (a.Mp / 32 + 3) / 4) <= 256) {
+    if (one && a.state && BH * (1 + (a.Mp / 32 + 3) / 4) <= 384) {
       if constexpr (lds + 49152 > 65536)
         (void)hipFuncSetAttribute(reinterpret_cast<const void*>(&k_decay_short<TX, DK, NT, NP, ELU>),
                                   hipFuncAttributeMaxDynamicSharedMemorySize, lds);
