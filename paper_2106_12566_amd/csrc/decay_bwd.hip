@@ -11,6 +11,12 @@
 // (SIDE 0) first sums its rows' numerators and denominators like the forward
 // pass and leaves G behind for the sums backwards in time and for the keys'
 // side (SIDE 1), whose first sums are dv.
+//
+// Bound by waits at one wave a SIMD in fp32 (204 registers, 150 KB of LDS) and two in bf16.  d = 64, n
+// rows of a head and the terms' products counted: 24 heads, n = 4096, 128 features, fp32 (60 M d +
+// 1920 (M + d) operations a row and side) 181 us a side, 0.47 PFLOP/s; 192 heads, n = 512, 64 features,
+// bf16 (34 M d + 960 M + 800 d) 62 us, 0.40 PFLOP/s (a large bf16 product of the library 1.22).  Two
+// work-groups a CU took bf16 from 79 us a side to 60; fp32 has no room for a second.
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
@@ -475,7 +481,7 @@ __global__ __launch_bounds__(256, sizeof(TX) == 2 && DK <= 4 ? 2 : 1) void k_dec
       for (int e = 0; e < 16; ++e) df[e] = fmaf(sden[8 * (e >> 2) + 4 * lh + (e & 3)], one, df[e]);
     }
     lo = zero16();
-      project_terms<DK, NSX, NW, false, WHOLE>(weights, own_rows, acc, lo);
+    project_terms<DK, NSX, NW, false, WHOLE>(weights, own_rows, acc, lo);
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
       const int l = 8 * (e >> 2) + 4 * lh + (e & 3);

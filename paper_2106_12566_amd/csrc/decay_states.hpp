@@ -28,7 +28,14 @@ __device__ __forceinline__ int path_rows(const int* __restrict__ path, int P, in
 
 // A wave owns 32 features, its sums in registers (lane: feature; value columns along the
 // registers), and its W; the rows of x and v pass through LDS for all waves of the work-group,
-// 32 PB of them at a time and fetched that far ahead.
+// 32 PB of them at a time and fetched that far ahead.  (Rows in every wave's registers instead
+// would be read once for each 32 features, and the sums in LDS would pass through it for each 32 rows.)
+//
+// Bound by waits between the matrix products: two waves a SIMD (the sums, W and the rows
+// ahead take 250 registers), where the projection, exp, the split into terms and the product of a
+// block follow each other.  d = 64: 96 heads, n = 4096, 128 features, fp32 (18 M d operations a row with
+// the terms' products) 125 us, 0.46 PFLOP/s; 16 heads, n = 16384, 256 features, bf16 (12 M d) 88 us,
+// 0.59 PFLOP/s; a large bf16 product of the library 1.22.  Three waves a SIMD spill.
 // NP, NV: terms of the features and of the values.
 template <typename TX, typename TV, int DK, int NP, int NV, bool ELU, Sums MODE, int WAVES>
 __device__ __forceinline__ void decay_states(const DecayArgs& a, int bh, int seg, int group) {
@@ -232,7 +239,8 @@ __global__ __launch_bounds__(64 * WAVES, DK <= 4 || (DK == 6 && WAVES == 4 && si
 }
 
 // The state before each segment (kBack: after it) in place of the segment's sums, and the one
-// behind the sequence: A <- e^{-rate rows} A + sums, one thread an element.
+// behind the sequence: A <- e^{-rate rows} A + sums, one thread an element.  Bound by the latency of
+// eight reads at a time: 96 heads of 65 x 128, 5 segments 11 us (32 MB), 16 of 65 x 256, 16 segments 8 us.
 template <bool BACK>
 __global__ __launch_bounds__(256) void k_decay_join(DecayArgs a) {
   const int bh = blockIdx.x, b = bh / a.H, h = bh % a.H;
