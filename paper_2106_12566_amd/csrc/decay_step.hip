@@ -10,21 +10,23 @@ namespace krpe {
 
 typedef unsigned uintx4 __attribute__((ext_vector_type(4)));
 // Four cells of a state's row c from feature l through its buffer: what lies past the last row or the
-// row's end (M) reads as zero and is not written.
+// row's end (M) reads as zero and is not written.  NT: past the caches (the non-temporal bit).
+template <bool NT>
 __device__ __forceinline__ float4 load_cells(const Rows<float>& st, int c, int l, bool vec) {
   const uint32_t o = l < st.d ? st.at(c) + 4u * l : kOut;
   if (vec) {
-    const uint4 u = st.b128(o);
+    const uint4 u = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(st.r, o, 0, NT ? 2 : 0));
     return make_float4(__uint_as_float(u.x), __uint_as_float(u.y), __uint_as_float(u.z), __uint_as_float(u.w));
   }
   return make_float4(st.one(o), st.one(l + 1 < st.d ? o + 4 : kOut), st.one(l + 2 < st.d ? o + 8 : kOut),
                      st.one(l + 3 < st.d ? o + 12 : kOut));
 }
+template <bool NT>
 __device__ __forceinline__ void store_cells(const Rows<float>& st, int c, int l, bool vec, float4 v) {
   const uint32_t o = l < st.d ? st.at(c) + 4u * l : kOut;
   const uintx4 u = {__float_as_uint(v.x), __float_as_uint(v.y), __float_as_uint(v.z), __float_as_uint(v.w)};
   if (vec) {
-    __builtin_amdgcn_raw_buffer_store_b128(u, st.r, o, 0, 0);
+    __builtin_amdgcn_raw_buffer_store_b128(u, st.r, o, 0, NT ? 2 : 0);
   } else {
 #pragma unroll
     for (int t = 0; t < 4; ++t) __builtin_amdgcn_raw_buffer_store_b32(u[t], st.r, l + t < st.d ? o + 4 * t : kOut, 0, 0);
@@ -37,10 +39,11 @@ __device__ __forceinline__ void store_cells(const Rows<float>& st, int c, int l,
 // (256 of them at a time), and a thread K rows at a time: the first K are asked for before the
 // token's features are worked out.  K sums over L lanes take fewer than K + log2(L) exchanges,
 // halving at each the rows that a lane has a part of.
-// 256 x 16 heads, 256 features, d = 64 (545 MB): 119 us, 4.6 TB/s (d = 128: 5.0; a plain copy 5.1).
-// With the state read after the features and a row summed at a time 142 us; with 8 or 16 rows at a
-// time 129 and 186 us and with six waves a SIMD 149 us, as registers run short.
-template <typename TX, int L, bool ELU>
+// 256 x 16 heads, 256 features, d = 64 (545 MB): 129 us, 4.2 TB/s, of states in memory (a plain copy 5.1).
+// The same states again and again, partly from the cache: 119; with the state read after the features
+// and a row summed at a time 142, with 8 or 16 rows at a time 129 and 186, with six waves a SIMD 149, as
+// registers run short.
+template <typename TX, int L, bool ELU, bool NT>
 __global__ __launch_bounds__(256, 4) void k_decay_step(PoolArgs a) {
   constexpr int K = 4, R = 256 / L;  // rows of a thread at a time, rows side by side
   extern __shared__ __align__(16) float sm[];
@@ -56,7 +59,7 @@ __global__ __launch_bounds__(256, 4) void k_decay_step(PoolArgs a) {
   float4 u[K];
   auto fetch = [&](int l, int p) {
 #pragma unroll
-    for (int i = 0; i < K; ++i) u[i] = load_cells(st, (p * K + i) * R + r0, l, vec);
+    for (int i = 0; i < K; ++i) u[i] = load_cells<NT>(st, (p * K + i) * R + r0, l, vec);
   };
   float sq = 0.f, sk = 0.f;  // squares of the rows, over each wave by itself
   for (int c = threadIdx.x & 63; c < d; c += 64) {
@@ -115,7 +118,7 @@ __global__ __launch_bounds__(256, 4) void k_decay_step(PoolArgs a) {
         const float y = c <= d ? v[c] : 0.f;
         u[i].x = fmaf(w, u[i].x, y * gk.x), u[i].y = fmaf(w, u[i].y, y * gk.y);
         u[i].z = fmaf(w, u[i].z, y * gk.z), u[i].w = fmaf(w, u[i].w, y * gk.w);
-        if (slot >= 0) store_cells(st, c, l, vec, u[i]);
+        if (slot >= 0) store_cells<NT>(st, c, l, vec, u[i]);
         s[i] = fmaf(u[i].x, gq.x, fmaf(u[i].y, gq.y, fmaf(u[i].z, gq.z, u[i].w * gq.w)));
       }
       // lane bit by lane bit, the half of the rows that stays takes the other lane's parts
@@ -196,14 +199,25 @@ void step(const PoolArgs& a, hipStream_t st) {
   const int M4 = (a.M + 3) & ~3, d4 = (a.d + 3) & ~3;
   const dim3 grid(static_cast<unsigned>(a.B) * a.H), block(256);
   const size_t lds = (4 * d4 + 2 * M4 + 8) * sizeof(float);
+  // States that the last-level cache of 256 MiB does not hold go past it.  16 heads, 256 features,
+  // d = 64, us with and without: 512 sequences (545 MB) 221 and 236; 256 (273 MB) 129 and 135 from memory,
+  // 117 and 108 where the call before left part of them in the cache; 192 (204 MB) 90 and 69.
+  const bool past = static_cast<size_t>(a.B) * a.H * (a.d + 1) * a.M * sizeof(float) > (size_t{256} << 20);
+  auto go = [&](auto lanes) {
+    constexpr int L = decltype(lanes)::value;
+    if (past)
+      hipLaunchKernelGGL((k_decay_step<TX, L, ELU, true>), grid, block, lds, st, a);
+    else
+      hipLaunchKernelGGL((k_decay_step<TX, L, ELU, false>), grid, block, lds, st, a);
+  };
   if (M4 <= 32)
-    hipLaunchKernelGGL((k_decay_step<TX, 8, ELU>), grid, block, lds, st, a);
+    go(std::integral_constant<int, 8>{});
   else if (M4 <= 64)
-    hipLaunchKernelGGL((k_decay_step<TX, 16, ELU>), grid, block, lds, st, a);
+    go(std::integral_constant<int, 16>{});
   else if (M4 <= 128)
-    hipLaunchKernelGGL((k_decay_step<TX, 32, ELU>), grid, block, lds, st, a);
+    go(std::integral_constant<int, 32>{});
   else
-    hipLaunchKernelGGL((k_decay_step<TX, 64, ELU>), grid, block, lds, st, a);
+    go(std::integral_constant<int, 64>{});
 }
 }  // namespace
 

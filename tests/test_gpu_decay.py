@@ -271,6 +271,21 @@ def test_step(gpu_lib, B, H, d, m, dt, features, nprf):
             assert ref.excess(c.state[s, h], last, lscale, torch.float32, ref.STATE_DELTA) <= 1.0
 
 
+def test_step_of_states_past_the_cache(gpu_lib):
+    """More than 256 MiB of states, beside the same in two halves."""
+    _say("step past the cache")
+    for d, m, B in ((64, 256, 260), (30, 77, 1900)):
+        c = Case(B, 16, 1, d, m, "bf16")
+        token = [x[:, :, 0].contiguous() for x in (c.q, c.k, c.v)]
+        halves = c.state.clone()
+        z = gpu_lib.decay_attention_step(*token, c.rate, c.W, c.state)
+        at = B // 2
+        for part in (slice(0, at), slice(at, B)):
+            y = gpu_lib.decay_attention_step(*(x[part] for x in token), c.rate, c.W, halves[part])
+            assert torch.equal(y, z[part])
+        assert torch.equal(halves, c.state)
+
+
 def _random_tree(rng, T):
     return [-1] + [int(rng.integers(-1, t)) for t in range(1, T)]
 
