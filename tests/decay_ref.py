@@ -16,9 +16,13 @@ F64 = torch.float64
 # roundings of its product, its constant and their sum, at most 3 x 40 x 2^-24 = 7e-6 of phi for q
 # and as much for k; sums of up to 256 terms in a register and between chunks add
 # 2^-24 sqrt(256) and less: 4e-5 covers twice the total.
-# bf16 results: operands in one term are off by 2^-8 of themselves at most: phi(q), phi(k) and
-# the state (or, in the gradients, W and the weights R): 4 x 2^-8 with what fp32 results have.
-DELTA = {torch.float32: 4e-5, torch.bfloat16: 4 * 2.0 ** -8}
+# bf16 results: phi(q) and phi(k) are operands of one term, off by 2^-8 of themselves at most; the
+# exponents carry W's two terms, 2^-17 |W| |x| <= 22 x 2^-17 for q and for k, and P and the state two
+# terms, 2^-16 each: 2 x 2^-8 + 4.5e-4 with what fp32 results have, below 2.2 x 2^-8.
+# Gradients of bf16 rows: all that is computed (phi(q), phi(k), the state, G, R, W) has two terms:
+# 6 x 2^-16 + 3.4e-4 + 4e-5 = 4.7e-4, below 2^-11; twice that for the two sums that dq and dk go through.
+DELTA = {torch.float32: 4e-5, torch.bfloat16: 2.2 * 2.0 ** -8}
+GRAD_DELTA = {torch.float32: 4e-5, torch.bfloat16: 2.0 ** -10}
 ROUND = {torch.float32: 2.0 ** -24, torch.bfloat16: 2.0 ** -8}  # half a step of the result's own type
 STATE_DELTA = 4e-5  # states are fp32 results in either case
 
