@@ -344,11 +344,15 @@ krpe_status_t krpe_attention_fwd_stats(const void* ws, size_t ws_bytes, int B, i
  * KRPE_STATE_FRESH (krpe_decay_fwd): sequences start from zeros; their slots are written only.
  */
 #define KRPE_STATE_FRESH 64u
+/*
+ * KRPE_ZERO_TAIL (krpe_decay_fwd, krpe_decay_bwd): the outputs' rows behind lens are zeros.
+ */
+#define KRPE_ZERO_TAIL 128u
 
 /*
  * Prompts: z [B, H, n, d] of q, k, v [B, H, n, d], in chunks of 128 positions.
  * lens  : [B] int32 (device) or NULL: sequence b has min(max(lens[b], 0), n) positions; z
- *         rows behind them stay as they were, q, k, v rows behind them weigh nothing.
+ *         rows behind them stay as they were (or KRPE_ZERO_TAIL), q, k, v rows behind them weigh nothing.
  * state : pool read before (not with KRPE_STATE_FRESH) and left as the states behind the
  *         sequences, or NULL (zeros before, not kept; slots must be NULL and nslots 0).
  * n == 0 is valid (it clears the slots with KRPE_STATE_FRESH).
@@ -361,7 +365,7 @@ krpe_status_t krpe_decay_fwd(const void* q, const void* k, const void* v, int qk
 
 /*
  * Backward pass of krpe_decay_fwd from zero states, W and rate fixed: dq, dk, dv [B, H, n, d] of
- * L = sum(dz * z), all in qkv_dtype.  Rows behind lens stay as they were.  The forward pass is
+ * L = sum(dz * z), all in qkv_dtype.  Rows behind lens stay as they were (or KRPE_ZERO_TAIL).  The forward pass is
  * recomputed inside.
  */
 size_t krpe_decay_bwd_workspace(int B, int H, int n, int d, int m, unsigned flags);

@@ -123,7 +123,7 @@ using namespace krpe;
 extern "C" {
 
 size_t krpe_decay_fwd_workspace(int B, int H, int n, int d, int m, unsigned flags) {
-  if (check_sizes(B, H, n, d, m, flags, kFlags | KRPE_STATE_FRESH) != KRPE_OK) return 0;
+  if (check_sizes(B, H, n, d, m, flags, kFlags | KRPE_STATE_FRESH | KRPE_ZERO_TAIL) != KRPE_OK) return 0;
   return decay_layout(static_cast<long long>(B) * H, n, d, m, 0).total;
 }
 
@@ -132,7 +132,7 @@ krpe_status_t krpe_decay_fwd(const void* q, const void* k, const void* v, int qk
                              int B, int H, int n, int d, int m, unsigned flags, void* ws, size_t ws_bytes,
                              void* stream) {
   clear_error();
-  if (krpe_status_t s = check_sizes(B, H, n, d, m, flags, kFlags | KRPE_STATE_FRESH)) return s;
+  if (krpe_status_t s = check_sizes(B, H, n, d, m, flags, kFlags | KRPE_STATE_FRESH | KRPE_ZERO_TAIL)) return s;
   if (krpe_status_t s = check_dtype(qkv_dtype)) return s;
   if (!state && (slots || nslots)) return fail(KRPE_ERR_NULL, "slots without a pool of states");
   if (!state && (flags & KRPE_STATE_FRESH)) return fail(KRPE_ERR_NULL, "KRPE_STATE_FRESH without a pool of states");
@@ -166,12 +166,13 @@ krpe_status_t krpe_decay_fwd(const void* q, const void* k, const void* v, int qk
   a.pre = reinterpret_cast<float*>(w + L.pre);
   a.B = B, a.H = H, a.n = n, a.d = d, a.M = m, a.Mp = L.Mp, a.nchunk = L.nchunk, a.nseg = L.nseg, a.segc = L.segc;
   a.nslots = nslots, a.nprf = (flags & KRPE_NPRF) != 0, a.fresh = (flags & KRPE_STATE_FRESH) != 0;
+  a.tail = lens && (flags & KRPE_ZERO_TAIL);
   a.log2_m = -0.5 * std::log2(static_cast<double>(m));
   return hip_check(launch_decay_fwd(qkv_dtype == KRPE_BF16, elu, a, static_cast<hipStream_t>(stream)), "decay launch");
 }
 
 size_t krpe_decay_bwd_workspace(int B, int H, int n, int d, int m, unsigned flags) {
-  if (check_sizes(B, H, n, d, m, flags, kFlags) != KRPE_OK) return 0;
+  if (check_sizes(B, H, n, d, m, flags, kFlags | KRPE_ZERO_TAIL) != KRPE_OK) return 0;
   return bwd_offsets(static_cast<long long>(B) * H, n, d, m).total;
 }
 
@@ -179,7 +180,7 @@ krpe_status_t krpe_decay_bwd(const void* q, const void* k, const void* v, int qk
                              const float* W, const void* dz, void* dq, void* dk, void* dv, const int* lens, int B,
                              int H, int n, int d, int m, unsigned flags, void* ws, size_t ws_bytes, void* stream) {
   clear_error();
-  if (krpe_status_t s = check_sizes(B, H, n, d, m, flags, kFlags)) return s;
+  if (krpe_status_t s = check_sizes(B, H, n, d, m, flags, kFlags | KRPE_ZERO_TAIL)) return s;
   if (krpe_status_t s = check_dtype(qkv_dtype)) return s;
   const long long bh = static_cast<long long>(B) * H;
   if (bh * n == 0) return KRPE_OK;
@@ -209,7 +210,7 @@ krpe_status_t krpe_decay_bwd(const void* q, const void* k, const void* v, int qk
   a.totb = reinterpret_cast<float*>(w + o.totb), a.preb = reinterpret_cast<float*>(w + o.preb);
   a.g = reinterpret_cast<float*>(w + o.g), a.gd = reinterpret_cast<float*>(w + o.gd);
   a.B = B, a.H = H, a.n = n, a.d = d, a.M = m, a.Mp = o.f.Mp, a.nchunk = o.f.nchunk, a.nseg = o.f.nseg, a.segc = o.f.segc;
-  a.nprf = (flags & KRPE_NPRF) != 0;
+  a.nprf = (flags & KRPE_NPRF) != 0, a.tail = lens && (flags & KRPE_ZERO_TAIL);
   a.log2_m = -0.5 * std::log2(static_cast<double>(m));
   return hip_check(launch_decay_bwd(qkv_dtype == KRPE_BF16, elu, a, static_cast<hipStream_t>(stream)),
                    "decay backward launch");

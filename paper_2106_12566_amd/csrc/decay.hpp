@@ -488,6 +488,12 @@ __device__ __forceinline__ void stage_columns(const Rows<TX>& x, uint4* __restri
   t.template put<NT, MODE>(vf, odd);
 }
 
+// Rows [r0, r1) of an array [.][d] cleared by a work-group of 256 threads.
+template <typename TZ>
+__device__ __forceinline__ void clear_rows(TZ* __restrict__ z, int r0, int r1, int d) {
+  for (int e = r0 * d + static_cast<int>(threadIdx.x); e < r1 * d; e += 256) z[e] = TZ{};
+}
+
 // ---- the prompts' passes
 struct DecayArgs {
   const void *q, *k, *v;
@@ -505,7 +511,7 @@ struct DecayArgs {
   const void* dz;
   void *dq, *dk, *dv;
   float *g, *gd, *totb, *preb;
-  int B, H, n, d, M, Mp, nchunk, nseg, segc, nslots, nprf, fresh, P;
+  int B, H, n, d, M, Mp, nchunk, nseg, segc, nslots, nprf, fresh, P, tail;  // tail: rows behind lens are cleared
   double log2_m;
 };
 __device__ __forceinline__ int rows_of(const int* __restrict__ lens, int b, int n) {

@@ -174,6 +174,11 @@ __global__ __launch_bounds__(256, sizeof(TX) == 2 && DK <= 4 ? 2 : 1) void k_dec
   const int lr = lane & 31, lh = lane >> 5;
   const int ch = blockIdx.x % a.nchunk, bh = blockIdx.x / a.nchunk, b = bh / a.H, h = bh % a.H, d = a.d;
   const int p0 = ch * kChunk, rows = rows_of(a.lens, b, a.n), cnt = min(kChunk, rows - p0);
+  if (a.tail) {
+    const size_t at = (static_cast<size_t>(bh) * a.n + p0) * d;
+    clear_rows(static_cast<TX*>(SIDE == 0 ? a.dq : a.dk) + at, max(cnt, 0), min(kChunk, a.n - p0), d);
+    if (SIDE == 1) clear_rows(static_cast<TX*>(a.dv) + at, max(cnt, 0), min(kChunk, a.n - p0), d);
+  }
   if (cnt <= 0) return;
   const size_t base = static_cast<size_t>(bh) * a.n * d, cells = static_cast<size_t>(d + 1) * a.Mp;
   const float rl = rate_log2(a.rate[h]);

@@ -43,6 +43,8 @@ __device__ __forceinline__ void decay_out(const DecayArgs& a, int block) {
   const int lr = lane & 31, lh = lane >> 5;
   const int ch = block % a.nchunk, bh = block / a.nchunk, b = bh / a.H, h = bh % a.H, d = a.d;
   const int p0 = ch * kChunk, rows = rows_of(a.lens, b, a.n), cnt = min(kChunk, rows - p0);
+  if (a.tail)
+    clear_rows(static_cast<TX*>(a.z) + (static_cast<size_t>(bh) * a.n + p0) * d, max(cnt, 0), min(kChunk, a.n - p0), d);
   if (cnt <= 0) return;
   const int slot = a.state ? slot_of(a.slots, b, a.B, a.nslots) : kStateNone;
   const size_t base = static_cast<size_t>(bh) * a.n * d, cells = static_cast<size_t>(d + 1) * a.Mp;

@@ -46,6 +46,7 @@ ROUTE_FFT = 16  # option bit: the FFT route of Section 3.2
 ROUTES = {"auto": 0, "direct": ROUTE_DIRECT, "fft": ROUTE_FFT}
 HINT_CAUSAL = 32  # option bit: b is -inf for every t > 0 (read by the route choice only)
 STATE_FRESH = 64  # option bit of decay_attention_fwd: sequences start from zeros
+ZERO_TAIL = 128  # option bit of decay_attention_fwd and _bwd: rows behind lens are zeros
 TREE_MAX, COPY_MAX = 64, 256  # nodes of a tree, moves of a copy
 
 
@@ -439,10 +440,10 @@ def _at(t: torch.Tensor | None) -> int | None:
     return None if t is None else t.data_ptr()
 
 
-def _like(out: torch.Tensor | None, x: torch.Tensor, zeros: bool) -> torch.Tensor:
+def _like(out: torch.Tensor | None, x: torch.Tensor) -> torch.Tensor:
     """The output beside input x: the one given, checked, or a new one."""
     if out is None:
-        return torch.zeros_like(x) if zeros else torch.empty_like(x)
+        return torch.empty_like(x)
     if not isinstance(out, torch.Tensor) or out.shape != x.shape or out.dtype != x.dtype or not out.is_contiguous():
         raise KrpeError("out must be a contiguous tensor of q's shape and dtype")
     if out.device != x.device:
@@ -490,7 +491,8 @@ def decay_attention_fwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, rate:
     elif slots is not None or fresh:
         raise KrpeError("slots and fresh need a state")
     slots, lens = _ints(slots, "slots", (B,), dev), _ints(lens, "lens", (B,), dev)
-    z = _like(out, q, lens is not None)
+    flags |= ZERO_TAIL if out is None and lens is not None else 0
+    z = _like(out, q)
     ws = _space(workspace, int(load().krpe_decay_fwd_workspace(B, H, n, d, m, flags)), dev)
     _enqueue("krpe_decay_fwd", dev, _at(q), _at(k), _at(v), DTYPES[q.dtype], _at(rate), _at(W), _at(z),
              _at(state), _at(slots), nslots, _at(lens), B, H, n, d, m, flags, ws.data_ptr(), ws.numel())
@@ -510,7 +512,8 @@ def decay_attention_bwd(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, rate:
     (q, k, v, dz), rate, W, m, shape, dev = _decay_inputs(("q", "k", "v", "dz"), (q, k, v, dz), rate, W, features, 4)
     B, H, n, d = shape
     lens = _ints(lens, "lens", (B,), dev)
-    dq, dk, dv = (_like(None, q, lens is not None) for _ in range(3))
+    flags |= ZERO_TAIL if lens is not None else 0
+    dq, dk, dv = (torch.empty_like(q) for _ in range(3))
     ws = _space(workspace, int(load().krpe_decay_bwd_workspace(B, H, n, d, m, flags)), dev)
     _enqueue("krpe_decay_bwd", dev, _at(q), _at(k), _at(v), DTYPES[q.dtype], _at(rate), _at(W), _at(dz),
              _at(dq), _at(dk), _at(dv), _at(lens), B, H, n, d, m, flags, ws.data_ptr(), ws.numel())
@@ -527,7 +530,7 @@ def decay_attention_step(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, rate
     B, H, d = shape
     nslots = _pool(state, H, d, m, dev)
     slots = _ints(slots, "slots", (B,), dev)
-    z = _like(out, q, False)
+    z = _like(out, q)
     _enqueue("krpe_decay_step", dev, _at(q), _at(k), _at(v), DTYPES[q.dtype], _at(rate), _at(W), _at(z),
              _at(state), _at(slots), nslots, B, H, d, m, flags)
     return z
@@ -547,7 +550,7 @@ def decay_attention_tree(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, pare
     if parent is None:
         raise KrpeError("parent must be int32 [B, T]")
     parent, slots = _ints(parent, "parent", (B, T), dev), _ints(slots, "slots", (B,), dev)
-    z = _like(out, q, False)
+    z = _like(out, q)
     _enqueue("krpe_decay_tree", dev, _at(q), _at(k), _at(v), DTYPES[q.dtype], _at(parent), _at(rate), _at(W),
              _at(z), _at(state), _at(slots), nslots, B, H, T, d, m, flags)
     return z

@@ -39,7 +39,7 @@ def test_fwd(lib):
     assert call(d=129) == UNSUP and call(m=1025) == UNSUP and call(n=1 << 30) == UNSUP
     assert call(B=1 << 12, H=1 << 12, n=1) == UNSUP    # more chunks than a grid has groups
     assert call(B=1, H=1, n=(1 << 31) - 1) == UNSUP and call(B=1, H=1, n=(1 << 31) - 129, wb=0) == WS
-    assert call(flags=2) == UNSUP and call(flags=8) == UNSUP and call(flags=16) == UNSUP and call(flags=128) == UNSUP
+    assert call(flags=2) == UNSUP and call(flags=8) == UNSUP and call(flags=16) == UNSUP and call(flags=256) == UNSUP
     assert call(flags=4) == SHAPE                      # elu + 1 needs m == d
     assert call(dt=2) == DTYPE
     assert call(ws=None) == WS and call(wb=need - 1) == WS

@@ -170,6 +170,23 @@ def test_lens(gpu_lib, dt):
                 assert ref.excess(got[b, h, :x], *g[name], got.dtype, ref.GRAD_DELTA[got.dtype]) <= 1.0, name
 
 
+@pytest.mark.parametrize("n,d", [(40, 7), (300, 24), (513, 72)])
+def test_rows_behind_lens_are_cleared(gpu_lib, n, d):
+    """Outputs in memory that held something else, one chunk or more, with and without a state."""
+    _say("cleared rows", n, d)
+    lens = [0, 1, n // 2, n]
+    c = Case(4, 3, n, d, 33, "bf16")
+    ln = torch.tensor(lens, dtype=torch.int32, device="cuda")
+    for with_state in (False, True):
+        for _ in range(2):
+            junk = [torch.full_like(c.q, 7.0) for _ in range(6)]
+            del junk
+            outs = [gpu_lib.decay_attention_fwd(c.q, c.k, c.v, c.rate, c.W, lens=ln, state=c.state if with_state else None),
+                    *gpu_lib.decay_attention_bwd(c.q, c.k, c.v, c.rate, c.W, c.dz, lens=ln)]
+            for b, x in enumerate(lens):
+                assert all(bool((o[b, :, x:] == 0).all()) and bool(o[b].isfinite().all()) for o in outs)
+
+
 def test_empty_prompts(gpu_lib):
     _say("n = 0")
     c = Case(2, 2, 0, 8, 16, slots=4)
